@@ -61,7 +61,13 @@ typedef struct hag_handle hag_t; /* opaque; immutable after construction except 
 /* Table 1, set Aggregate.  HAG_GCN is the GCN row's Update up to the weight matrix, fused
  * into the aggregation: y[v] = (sum over N(v) of x[u] + x[v]) / (|N(v)| + 1); f32 only. */
 typedef enum { HAG_SUM = 0, HAG_MEAN = 1, HAG_MAX = 2, HAG_GCN = 3 } hag_op_t;
-typedef enum { HAG_F32 = 0, HAG_I32 = 1 } hag_dtype_t;
+typedef enum {
+    HAG_F32 = 0,
+    HAG_I32 = 1,
+    HAG_BF16 = 2, /* lookups, layer norm and clipping only, as are ... */
+    HAG_F16 = 3,
+    HAG_I64 = 4 /* ... 64-bit ids */
+} hag_dtype_t;
 
 enum {
     HAG_OK = 0,
@@ -394,6 +400,46 @@ int hag_softmax_loss(int64_t n, int64_t classes, const float *z, const int64_t *
                      void *workspace, void *stream);
 int hag_softmax_loss_grad(int64_t n, int64_t classes, const float *z, const int64_t *labels, int64_t ignore, const float *counted,
                           const float *g_loss, float *g_z, void *stream);
+
+/* What feeds and steadies the training of a model whose nodes carry an id or a category (a degree, a label) instead of a feature row.  Device pointers; kernels
+ * only, so they can be captured; elements HAG_F32, HAG_BF16 or HAG_F16 at any address that suits one element, sums and statistics in fp32 or wider, each
+ * result rounded once.  Inputs are matrices with contiguous rows and a row stride in elements (0: the same row throughout), outputs are contiguous; n and the
+ * number of rows of a table are below 2^31, d is in 1 .. 2^20.  `workspace` is 16-byte aligned, of the bytes that the function above the call names.
+ *
+ * hag_embedding: y [n, d] = scale * table[ids], table [rows, d], ids [n] (HAG_I32 or HAG_I64).  An id equal to `padding` gives a row of zeros whatever the table
+ * holds (HAG_NO_PADDING: there is none), any other id that is no row of the table a row of NaN.
+ * hag_embedding_grad: g_table [rows, d] = scale * the sum of the rows of g_y [n, d] whose id names the row, 0 for rows that none names; g_table has the
+ * type of g_y or HAG_F32.  Ids that are `padding` or no row send no gradient.  Fixed order of additions: the same bits every time.
+ *
+ * hag_layer_norm: y = (x - mean) * rstd * weight + bias per row of x [n, d]; mean [n], rstd [n] = 1 / sqrt(variance + eps) (either may be NULL: not kept), weight and
+ * bias [d] of the type of x or HAG_F32 (either may be NULL: 1 and 0).
+ * hag_layer_norm_grad: the gradients at x, weight and bias (the latter two of param_dtype; either may be NULL: not wanted) of a loss whose gradient
+ * at y is g_y, with mean and rstd as the forward call left them.  Fixed order of additions.
+ *
+ * hag_clip_gradients: *norm (fp32, device) = the 2-norm of all elements of all tensors as one vector, and out = in * (max_norm / norm where the norm is above
+ * max_norm, else 1) for each of them.  `list` is host memory, read during the call; out may be in (then nothing is written where nothing is clipped), else they must not overlap.
+ * Squares are added up in fp64 in a fixed order.  An infinite norm makes finite elements 0 and infinite ones NaN, a NaN makes all NaN; max_norm may be
+ * infinite.  Captured calls keep the addresses they were captured with. */
+#define HAG_NO_PADDING INT64_MIN
+int hag_embedding(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, const void *table, int64_t table_stride, hag_dtype_t id_type, const void *ids,
+                  int64_t padding, float scale, void *y, void *stream);
+size_t hag_embedding_grad_workspace_bytes(int64_t n, int64_t rows, int64_t d);
+int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, const void *g_y, int64_t g_y_stride, hag_dtype_t id_type, const void *ids, int64_t padding,
+                       float scale, hag_dtype_t out_dtype, void *g_table, void *workspace, void *stream);
+int hag_layer_norm(int64_t n, int64_t d, hag_dtype_t dtype, const void *x, int64_t x_stride, hag_dtype_t param_dtype, const void *weight, const void *bias, float eps, void *y,
+                   float *mean, float *rstd, void *stream);
+size_t hag_layer_norm_grad_workspace_bytes(int64_t n, int64_t d);
+int hag_layer_norm_grad(int64_t n, int64_t d, hag_dtype_t dtype, const void *g_y, int64_t g_y_stride, const void *x, int64_t x_stride, hag_dtype_t param_dtype, const void *weight,
+                        const float *mean, const float *rstd, void *g_x, void *g_weight, void *g_bias, void *workspace, void *stream);
+typedef struct hag_tensor {
+    const void *in;
+    void *out;
+    int64_t count;  /* elements */
+    int32_t dtype;  /* HAG_F32, HAG_BF16, HAG_F16 */
+    int32_t zero;   /* 0 */
+} hag_tensor_t;
+size_t hag_clip_workspace_bytes(int64_t tensors);
+int hag_clip_gradients(int64_t tensors, const hag_tensor_t *list, double max_norm, float *norm, void *workspace, void *stream);
 
 /* Algorithmic bytes one call moves (every HAG edge one row read, every produced
  * row one write, plus index reads), for roofline accounting.  which: 0 hag_forward,

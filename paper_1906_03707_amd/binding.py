@@ -8,6 +8,7 @@ symbol from it raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -17,7 +18,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("HAG_LIB", os.path.join(_HERE, "libhag.so"))
 
 HAG_SUM, HAG_MEAN, HAG_MAX, HAG_GCN = 0, 1, 2, 3
-HAG_F32, HAG_I32 = 0, 1
+HAG_F32, HAG_I32, HAG_BF16, HAG_F16, HAG_I64 = 0, 1, 2, 3, 4
+HAG_NO_PADDING = -1 << 63
 HAG_OK, HAG_EINVAL, HAG_ENOMEM, HAG_EHIP, HAG_ESTATE, HAG_ETIMEOUT = 0, -1, -2, -3, -4, -5
 HAG_OPT_ONE_LAUNCH_MAX_ITEMS, HAG_OPT_SPIN_LIMIT, HAG_OPT_TEST_WAIT_UNREACHABLE, HAG_OPT_DETERMINISTIC_MAX_BACKWARD = 1, 2, 3, 4
 HAG_OPT_SEQ_ONE_LAUNCH = 6
@@ -35,6 +37,8 @@ EXPORTS = [
     "hag_seq_create", "hag_seq_free", "hag_seq_cells", "hag_seq_ranks", "hag_seq_launches", "hag_seq_get_plan", "hag_seq_set_option", "hag_seq_check", "hag_seq_train_workspace_bytes", "hag_seq_lstm_forward_train", "hag_seq_lstm_backward", "hag_seq_merges", "hag_seq_upload", "hag_seq_workspace_bytes",
     "hag_seq_lstm_forward", "hag_seq_weight_grad_slabs", "hag_route", "hag_naive_route", "hag_forward_workspace_bytes",
     "hag_weight_grad_workspace_bytes", "hag_weight_grad", "hag_narrow_product", "hag_softmax_loss_workspace_bytes", "hag_softmax_loss", "hag_softmax_loss_grad",
+    "hag_embedding", "hag_embedding_grad_workspace_bytes", "hag_embedding_grad", "hag_layer_norm", "hag_layer_norm_grad_workspace_bytes", "hag_layer_norm_grad",
+    "hag_clip_workspace_bytes", "hag_clip_gradients",
 ]
 ROUTES = ("hag", "lists", "component_hag", "component_lists", "dense", "one_launch", "scatter")   # HAG_ROUTE_*
 HAG_STATIC_SCRATCH_BYTES = 64 << 20
@@ -125,6 +129,18 @@ def lib():
         L.hag_softmax_loss_workspace_bytes.restype = ctypes.c_size_t
         L.hag_softmax_loss.argtypes = [i64, i64, vp, vp, i64] + [vp] * 4
         L.hag_softmax_loss_grad.argtypes = [i64, i64, vp, vp, i64] + [vp] * 4
+        f32, size_t = ctypes.c_float, ctypes.c_size_t
+        L.hag_embedding.argtypes = [i64, i64, i64, i32, vp, i64, i32, vp, i64, f32, vp, vp]
+        L.hag_embedding_grad_workspace_bytes.argtypes = [i64, i64, i64]
+        L.hag_embedding_grad_workspace_bytes.restype = size_t
+        L.hag_embedding_grad.argtypes = [i64, i64, i64, i32, vp, i64, i32, vp, i64, f32, i32, vp, vp, vp]
+        L.hag_layer_norm.argtypes = [i64, i64, i32, vp, i64, i32, vp, vp, f32, vp, vp, vp, vp]
+        L.hag_layer_norm_grad_workspace_bytes.argtypes = [i64, i64]
+        L.hag_layer_norm_grad_workspace_bytes.restype = size_t
+        L.hag_layer_norm_grad.argtypes = [i64, i64, i32, vp, i64, vp, i64, i32] + [vp] * 8
+        L.hag_clip_workspace_bytes.argtypes = [i64]
+        L.hag_clip_workspace_bytes.restype = size_t
+        L.hag_clip_gradients.argtypes = [i64, vp, ctypes.c_double, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -473,6 +489,180 @@ def softmax_loss_grad(z, labels, counted, g_loss, ignore=-100):
     out = torch.empty_like(z)
     _check(lib().hag_softmax_loss_grad(n, classes, z.data_ptr(), labels.data_ptr(), int(ignore), _scalar(counted, z), _scalar(g_loss, z), out.data_ptr(), _raw_stream()))
     return out
+
+
+_elements = None
+
+
+def _element_codes():
+    """{torch dtype: HAG code} of what lookups, layer norm and clipping take."""
+    import torch
+    global _elements
+    _elements = {torch.float32: HAG_F32, torch.bfloat16: HAG_BF16, torch.float16: HAG_F16}
+    return _elements
+
+
+def _device():
+    return (_torch_calls or _resolve_torch_calls())[0]()
+
+
+def _rows(name, t, device):
+    """(element code, row stride) of a matrix with contiguous rows on the current device."""
+    code = (_elements or _element_codes()).get(t.dtype)
+    if code is None or t.dim() != 2 or t.get_device() != device:
+        raise ValueError(f"{name} must be a float32, bfloat16 or float16 matrix on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    n, d = t.shape
+    stride, step = t.stride()
+    if step != 1 and d > 1 and n > 0:
+        raise ValueError(f"the rows of {name} must be contiguous, got strides {tuple(t.stride())}")
+    return code, stride if n > 1 else d
+
+
+def _ids(ids, device):
+    import torch
+    if ids.dtype not in (torch.int64, torch.int32) or ids.get_device() != device or not ids.is_contiguous():
+        raise ValueError(f"ids must be contiguous int64 or int32 on the current device, got {ids.dtype} {tuple(ids.shape)} on {ids.device}")
+    return HAG_I64 if ids.dtype == torch.int64 else HAG_I32
+
+
+def embedding(table, ids, scale=1.0, padding=None):
+    """scale * table[ids] [*ids.shape, d] of a table [rows, d] (hag_embedding).  Ids equal to `padding` (any number, a row or not) give rows of zeros, ids that are
+    no row of the table rows of NaN."""
+    import torch
+    device = _device()
+    code, stride = _rows("table", table, device)
+    id_code, (rows, d) = _ids(ids, device), table.shape
+    y = torch.empty((*ids.shape, d), dtype=table.dtype, device=table.device)
+    rc = lib().hag_embedding(ids.numel(), rows, d, code, table.data_ptr(), stride, id_code, ids.data_ptr(), HAG_NO_PADDING if padding is None else int(padding), scale,
+                             y.data_ptr(), _raw_stream())
+    if rc != 0:
+        _check(rc)
+    return y
+
+
+def embedding_grad(g_y, ids, rows, scale=1.0, padding=None, dtype=None):
+    """Gradient [rows, d] at the table of embedding(table, ids, scale, padding), for the gradient g_y [n, d] at its rows, n = ids.numel() (hag_embedding_grad);
+    dtype: that of g_y (the default) or float32."""
+    import torch
+    device = _device()
+    code, stride = _rows("g_y", g_y, device)
+    id_code, (n, d) = _ids(ids, device), g_y.shape
+    if ids.numel() != n:
+        raise ValueError(f"g_y has {n} rows for {ids.numel()} ids")
+    if dtype is None:
+        dtype = g_y.dtype
+    elif dtype not in _elements:
+        raise ValueError(f"unsupported dtype {dtype}")
+    if rows < 0:
+        raise ValueError("rows must not be negative")
+    out = torch.empty((rows, d), dtype=dtype, device=g_y.device)
+    L = lib()
+    ws = torch.empty(L.hag_embedding_grad_workspace_bytes(n, rows, d), dtype=torch.uint8, device=g_y.device)
+    rc = L.hag_embedding_grad(n, rows, d, code, g_y.data_ptr(), stride, id_code, ids.data_ptr(), HAG_NO_PADDING if padding is None else int(padding), scale, _elements[dtype],
+                              out.data_ptr(), ws.data_ptr(), _raw_stream())
+    if rc != 0:
+        _check(rc)
+    return out
+
+
+def _norm_params(x, weight, bias):
+    """The element code of weight and bias, which have the type of x or are float32, and their addresses."""
+    code, ptrs = None, []
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is None:
+            ptrs.append(None)
+            continue
+        got = _elements.get(t.dtype)
+        if t.dim() != 1 or t.shape[0] != x.shape[1] or t.get_device() != x.get_device() or not t.is_contiguous() or code not in (None, got) \
+                or (got != HAG_F32 and t.dtype != x.dtype):
+            raise ValueError(f"{name} must have one contiguous element for each of the {x.shape[1]} columns, float32 or of the type of x, on its device; got {t.dtype} "
+                             f"{tuple(t.shape)} on {t.device}")
+        code = got
+        ptrs.append(t.data_ptr())
+    return HAG_F32 if code is None else code, ptrs
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """(y, mean, rstd) of x [n, d]: every row less its mean, over its standard deviation, times weight plus bias (hag_layer_norm)."""
+    import torch
+    code, stride = _rows("x", x, _device())
+    n, d = x.shape
+    param_code, (w, b) = _norm_params(x, weight, bias)
+    y = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    mean, rstd = torch.empty(n, dtype=torch.float32, device=x.device), torch.empty(n, dtype=torch.float32, device=x.device)
+    rc = lib().hag_layer_norm(n, d, code, x.data_ptr(), stride, param_code, w, b, eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _raw_stream())
+    if rc != 0:
+        _check(rc)
+    return y, mean, rstd
+
+
+def layer_norm_grad(g_y, x, mean, rstd, weight=None, params=True):
+    """(g_x, g_weight, g_bias): the gradients of layer_norm for the gradient g_y at y, mean and rstd as it returned them; the latter two of the type of weight
+    (float32 without one), None if not params (hag_layer_norm_grad)."""
+    import torch
+    device = _device()
+    code, stride = _rows("x", x, device)
+    g_code, g_stride = _rows("g_y", g_y, device)
+    if g_code != code or g_y.shape != x.shape:
+        raise ValueError(f"g_y must match x: {x.dtype} {tuple(x.shape)}, got {g_y.dtype} {tuple(g_y.shape)}")
+    n, d = x.shape
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or t.get_device() != device or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous float32, one for each of the {n} rows, on the current device")
+    param_code, (w, _) = _norm_params(x, weight, None)
+    g_x, g_w, g_b, ws = torch.empty((n, d), dtype=x.dtype, device=x.device), None, None, None
+    L = lib()
+    if params:
+        g_w, g_b = (torch.empty(d, dtype=torch.float32 if weight is None else weight.dtype, device=x.device) for _ in range(2))
+        ws = torch.empty(L.hag_layer_norm_grad_workspace_bytes(n, d), dtype=torch.uint8, device=x.device)
+    rc = L.hag_layer_norm_grad(n, d, code, g_y.data_ptr(), g_stride, x.data_ptr(), stride, param_code, w, mean.data_ptr(), rstd.data_ptr(), g_x.data_ptr(),
+                               *((g_w.data_ptr(), g_b.data_ptr(), ws.data_ptr()) if params else (None, None, None)), _raw_stream())
+    if rc != 0:
+        _check(rc)
+    return g_x, g_w, g_b
+
+
+def _dense(t):
+    """Its elements fill a piece of memory, in whatever order of the dimensions."""
+    if t.is_contiguous():
+        return True
+    count = 1
+    for stride, size in sorted((stride, size) for stride, size in zip(t.stride(), t.shape) if size != 1):
+        if stride != count:
+            return False
+        count *= size
+    return True
+
+
+def clip_gradients(tensors, max_norm, out=None):
+    """The 2-norm (float32, on the device) of all elements of `tensors` as one vector; where it is above max_norm they are scaled down to it, in place or into the
+    tensors of `out`, which get them unchanged where it is not (hag_clip_gradients).  The tensors fill their memory and do not overlap, each is float32, bfloat16 or float16."""
+    import torch
+    tensors = list(tensors)
+    outs = tensors if out is None else list(out)
+    if len(outs) != len(tensors):
+        raise ValueError(f"{len(outs)} outputs for {len(tensors)} tensors")
+    device, codes = _device(), _elements or _element_codes()
+    entries = array.array("q")
+    for t, o in zip(tensors, outs):
+        code = codes.get(t.dtype)
+        if code is None or t.get_device() != device or not _dense(t):
+            raise ValueError(f"dense float32, bfloat16 or float16 tensors on the current device are needed, got {t.dtype} {tuple(t.shape)} with strides {tuple(t.stride())} on {t.device}")
+        if o is not t and (o.dtype != t.dtype or o.shape != t.shape or o.get_device() != device or o.stride() != t.stride()):
+            raise ValueError(f"an output must match its tensor: {t.dtype} {tuple(t.shape)} with strides {tuple(t.stride())}, got {o.dtype} {tuple(o.shape)} with {tuple(o.stride())}")
+        count = t.numel()
+        if count:
+            entries.extend((t.data_ptr(), o.data_ptr(), count, code))
+    count = len(entries) // 4
+    if len(set(entries[1::4])) != count:
+        raise ValueError("a tensor is named twice")
+    norm = torch.empty((), dtype=torch.float32, device="cuda")
+    L = lib()
+    ws = torch.empty(L.hag_clip_workspace_bytes(count), dtype=torch.uint8, device="cuda")
+    rc = L.hag_clip_gradients(count, entries.buffer_info()[0], max_norm, norm.data_ptr(), ws.data_ptr(), _raw_stream())
+    if rc != 0:
+        _check(rc)
+    return norm
 
 
 def probe_rows(src, n_rows, d, reads, from_lds, workgroups, sink) -> int:

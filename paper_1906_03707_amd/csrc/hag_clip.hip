@@ -1,0 +1,138 @@
+// The 2-norm of many tensors taken as one vector, and all of them scaled so that it is at most max_norm.
+//   N = sqrt(sum of g^2),  c = N <= max_norm ? 1 : max_norm / N,  out = c g
+#include "hag_elem.hpp"
+
+#include <cmath>
+
+namespace hag {
+
+// The tensors are cut into units of at most `unit` elements, one workgroup each; a launch takes as many tensors as its argument block holds.
+constexpr int kClipTensors = 112, kClipUnits = 2048;
+struct ClipArgs {
+    struct Tensor {
+        const void *in;
+        void *out;
+        int64_t count;
+        int32_t dtype;
+        int32_t first_unit;      // of this launch
+    } t[kClipTensors];
+    int64_t unit;
+    int32_t tensors;
+    int32_t units;               // of this launch
+    int32_t partial_at;          // where this launch's units begin among those of all launches
+    int32_t partials;            // units of all launches
+};
+static_assert(sizeof(ClipArgs) <= 3840, "kernel arguments are limited to 4 KB");
+
+// the tensor of a unit: the last one that does not begin after it
+__device__ __forceinline__ int clip_tensor(const ClipArgs &a, int unit) {
+    int lo = 0, hi = a.tensors;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.t[mid].first_unit <= unit) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ double block_sum64(double v, double *lds) {
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) v += __shfl_xor(v, off);
+    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = 0.;
+#pragma unroll
+    for (int w = 0; w < kBlock / kWave; ++w) v += lds[w];
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ double sum_squares(const T *p, int64_t count) {
+    double s = 0.;
+    for (int64_t i = threadIdx.x; i < count; i += kBlock) { const double v = (double)(float)p[i]; s += v * v; }
+    return s;
+}
+
+// Squares are taken and added up in 64 bits: the square of an fp32 gradient above 2e19 is no fp32 number.
+__global__ __launch_bounds__(kBlock) void clip_sums_kernel(ClipArgs a, double *__restrict__ partial) {
+    __shared__ double lds[kBlock / kWave];
+    const int t = clip_tensor(a, blockIdx.x);
+    const int64_t begin = (int64_t)(blockIdx.x - a.t[t].first_unit) * a.unit, count = min(a.unit, a.t[t].count - begin);
+    const double s = a.t[t].dtype == HAG_F32    ? sum_squares((const float *)a.t[t].in + begin, count)
+                     : a.t[t].dtype == HAG_BF16 ? sum_squares((const bf16_t *)a.t[t].in + begin, count)
+                                                : sum_squares((const f16_t *)a.t[t].in + begin, count);
+    const double sum = block_sum64(s, lds);
+    if (threadIdx.x == 0) partial[a.partial_at + blockIdx.x] = sum;
+}
+
+template <typename T>
+__device__ __forceinline__ void scale_unit(const T *p, T *out, int64_t count, float c) {
+    for (int64_t i = threadIdx.x; i < count; i += kBlock) out[i] = (T)((float)p[i] * c);
+}
+
+__global__ __launch_bounds__(kBlock) void clip_scale_kernel(ClipArgs a, const double *__restrict__ partial, double max_norm, float *__restrict__ norm) {
+    __shared__ double lds[kBlock / kWave];
+    double s = 0.;
+    for (int i = threadIdx.x; i < a.partials; i += kBlock) s += partial[i];
+    const double total = sqrt(block_sum64(s, lds));
+    const float c = total <= max_norm ? 1.f : (float)(max_norm / total);   // (a NaN: NaN; an infinite norm: 0, and NaN for the infinite elements)
+    if (blockIdx.x == 0 && a.partial_at == 0 && threadIdx.x == 0) *norm = (float)total;
+    if ((int)blockIdx.x >= a.units) return;                // no element at all: the launch is there for the norm
+    const int t = clip_tensor(a, blockIdx.x);
+    if (c == 1.f && a.t[t].out == a.t[t].in) return;
+    const int64_t begin = (int64_t)(blockIdx.x - a.t[t].first_unit) * a.unit, count = min(a.unit, a.t[t].count - begin);
+    if (a.t[t].dtype == HAG_F32) scale_unit((const float *)a.t[t].in + begin, (float *)a.t[t].out + begin, count, c);
+    else if (a.t[t].dtype == HAG_BF16) scale_unit((const bf16_t *)a.t[t].in + begin, (bf16_t *)a.t[t].out + begin, count, c);
+    else scale_unit((const f16_t *)a.t[t].in + begin, (f16_t *)a.t[t].out + begin, count, c);
+}
+
+}  // namespace hag
+
+using namespace hag;
+
+extern "C" {
+
+// every tensor has at most one unit that is not full
+size_t hag_clip_workspace_bytes(int64_t tensors) { return tensors < 0 || tensors > (1 << 24) ? 0 : (size_t)(kClipUnits + tensors) * sizeof(double); }
+
+int hag_clip_gradients(int64_t tensors, const hag_tensor_t *list, double max_norm, float *norm, void *workspace, void *stream) {
+    if (tensors < 0 || tensors > (1 << 24)) { set_error("number of tensors must be in 0 .. 2^24"); return HAG_EINVAL; }
+    if (!(max_norm > 0.)) { set_error("max_norm must be positive"); return HAG_EINVAL; }
+    if ((tensors > 0 && !list) || !norm || !workspace) { set_error("NULL pointer"); return HAG_EINVAL; }
+    if ((uintptr_t)workspace & 15) { set_error("workspace must be 16-byte aligned"); return HAG_EINVAL; }
+    int64_t total = 0;
+    for (int64_t i = 0; i < tensors; ++i) {
+        const hag_tensor_t &t = list[i];
+        if (t.count < 0 || t.count > ((int64_t)1 << 48)) { set_error("count of a tensor out of range"); return HAG_EINVAL; }
+        if (!elem_type((hag_dtype_t)t.dtype)) { set_error("elements are HAG_F32, HAG_BF16 or HAG_F16"); return HAG_EINVAL; }
+        if (t.count > 0 && (!t.in || !t.out)) { set_error("NULL pointer"); return HAG_EINVAL; }
+        total += t.count;
+    }
+    const int64_t unit = std::max<int64_t>(4096, (total + kClipUnits - 1) / kClipUnits);
+    // the launches' argument blocks one after the other, first to add up, then to scale
+    hipStream_t s = (hipStream_t)stream;
+    int64_t partials = 0;
+    for (int64_t i = 0; i < tensors; ++i) partials += (list[i].count + unit - 1) / unit;
+    for (int pass = 0; pass < 2; ++pass) {
+        int64_t at = 0, i = 0;
+        do {
+            ClipArgs a;
+            a.unit = unit;
+            a.tensors = a.units = 0;
+            a.partial_at = (int32_t)at;
+            a.partials = (int32_t)partials;
+            for (; i < tensors && a.tensors < kClipTensors; ++i) {
+                if (list[i].count == 0) continue;
+                a.t[a.tensors++] = {list[i].in, list[i].out, list[i].count, list[i].dtype, a.units};
+                a.units += (int32_t)((list[i].count + unit - 1) / unit);
+            }
+            if (pass == 0 && a.units > 0) hipLaunchKernelGGL(clip_sums_kernel, dim3((unsigned)a.units), dim3(kBlock), 0, s, a, (double *)workspace);
+            if (pass == 1 && (a.units > 0 || at == 0))
+                hipLaunchKernelGGL(clip_scale_kernel, dim3((unsigned)std::max(a.units, 1)), dim3(kBlock), 0, s, a, (const double *)workspace, max_norm, norm);
+            HIP_TRY(hipGetLastError());
+            at += a.units;
+        } while (i < tensors);
+    }
+    return HAG_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,227 @@
+"""hag_layer_norm and hag_layer_norm_grad against the formulas in 64 bits: widths from one column to more than a workgroup holds, odd ones, views, rows without spread,
+gradients by differences, parameter gradients that see a lost row."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -24
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TINY = {torch.float32: 0.0, torch.bfloat16: 0.0, torch.float16: 2.0 ** -25}
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+WIDTHS = [1, 2, 3, 4, 7, 8, 16, 31, 36, 64, 100, 127, 128, 130, 251, 256, 260, 500, 512, 513, 777, 1024, 1030, 2048, 2050, 4096, 4099, 8192, 8200, 16500]
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1906_03707_amd import binding
+    binding.lib()
+    return binding
+
+
+def forward64(x, w, b, eps):
+    x = x.double()
+    m = x.mean(1, keepdim=True)
+    r = ((x - m).square().mean(1, keepdim=True) + eps).rsqrt()
+    xh = (x - m) * r
+    return xh * (1.0 if w is None else w.double()) + (0.0 if b is None else b.double()), m, r, xh
+
+
+def check_forward(got, x, w, b, eps):
+    y, mean, rstd = got
+    want, m, r, xh = forward64(x, w, b, eps)
+    n, d = x.shape
+    # mean: any order of d additions and a division; the deviations are from the mean as it came out
+    dm = (d + 2) * EPS * x.double().abs().mean(1, keepdim=True)
+    dr = r * ((d + 8) / 2 * EPS + 4 * EPS + (dm * r) ** 2 / 2)
+    dxh = r * (dm + EPS * (x.double() - m).abs()) + xh.abs() * dr / r
+    dy = dxh * (1.0 if w is None else w.double().abs()) + 3 * EPS * (xh.abs() * (1.0 if w is None else w.double().abs()) + (0.0 if b is None else b.double().abs()))
+    dy = dy + HALF[y.dtype] * (want.abs() + dy) + TINY[y.dtype]
+    assert y.dtype == x.dtype and mean.shape == rstd.shape == (n,)
+    assert bool(((mean.double()[:, None] - m).abs() <= dm).all())
+    assert bool(((rstd.double()[:, None] - r).abs() <= dr).all())
+    assert bool(((y.double() - want).abs() <= dy).all())
+
+
+def check_grad(got, gy, x, mean, rstd, w):
+    gx, gw, gb = got
+    n, d = x.shape
+    g, r = gy.double(), rstd.double()[:, None]
+    xh = (x.double() - mean.double()[:, None]) * r
+    u = g if w is None else g * w.double()
+    s1, s2 = u.mean(1, keepdim=True), (u * xh).mean(1, keepdim=True)
+    want = r * (u - s1 - xh * s2)
+    a1, a2 = u.abs().mean(1, keepdim=True), (u * xh).abs().mean(1, keepdim=True)
+    # xh carries two roundings, u one, their sums d additions more; then four operations on terms of these sizes
+    bound = r * (6 * EPS * u.abs() + (d + 6) * EPS * a1 + xh.abs() * ((d + 10) * EPS * a2 + 6 * EPS * s2.abs()) + 4 * EPS * s1.abs()) + 2 * EPS * want.abs()
+    bound = bound + HALF[gx.dtype] * (want.abs() + bound) + TINY[gx.dtype]
+    assert gx.dtype == x.dtype and bool(((gx.double() - want).abs() <= bound).all())
+    if gw is None:
+        return
+    for got_p, terms, extra in ((gw, g * xh, 4), (gb, g, 1)):
+        total, size = terms.sum(0), terms.abs().sum(0)
+        bound = (n + extra) * EPS * size
+        bound = bound + HALF[got_p.dtype] * (total.abs() + bound) + TINY[got_p.dtype]
+        assert bool(((got_p.double() - total).abs() <= bound).all())
+
+
+def params(d, dtype, gen):
+    return ((1 + 0.3 * torch.randn(d, device="cuda", generator=gen)).to(dtype), (0.2 * torch.randn(d, device="cuda", generator=gen)).to(dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", WIDTHS)
+def test_norm_and_gradient(B, d, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    for n in (1, 2, 5, 67, 1030) if d < 600 else (1, 3, 130):
+        x = (2 * torch.randn(n, d, device="cuda", generator=gen) + torch.randn(n, 1, device="cuda", generator=gen)).to(dtype)
+        gy = torch.randn(n, d, device="cuda", generator=gen).to(dtype)
+        for w, b in (params(d, torch.float32, gen), params(d, dtype, gen), (None, None)):
+            out = B.layer_norm(x, w, b)
+            check_forward(out, x, w, b, 1e-5)
+            check_grad(B.layer_norm_grad(gy, x, out[1], out[2], w), gy, x, out[1], out[2], w)
+    w, b = params(d, torch.float32, gen)
+    check_forward(B.layer_norm(x, w, None, eps=0.1), x, w, None, 0.1)
+    check_forward(B.layer_norm(x, None, b, eps=0.1), x, None, b, 0.1)
+    gx, gw, gb = B.layer_norm_grad(gy, x, out[1], out[2], w, params=False)
+    assert gw is None and gb is None
+    assert torch.equal(gx, B.layer_norm_grad(gy, x, out[1], out[2], w)[0])
+    assert all(torch.equal(p, q) for p, q in zip(B.layer_norm_grad(gy, x, out[1], out[2], w), B.layer_norm_grad(gy, x, out[1], out[2], w)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,d", [(70001, 16), (40000, 64), (30000, 100), (9001, 250), (5000, 1000), (3001, 3000), (600, 9000)])
+def test_parameter_gradients_count_every_row_once(B, n, d, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    x, gy = (torch.randint(-3, 4, (n, d), device="cuda", generator=gen).to(dtype) for _ in range(2))
+    zero, one = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda")
+    gx, gw, gb = B.layer_norm_grad(gy, x, zero, one)       # with these statistics all terms are whole numbers, their sums exact in fp32
+    assert torch.equal(gw.double(), (gy.double() * x.double()).sum(0)) and torch.equal(gb.double(), gy.double().sum(0))
+    check_grad((gx, None, None), gy, x, zero, one, None)
+
+
+@pytest.mark.parametrize("n,d", [(3, 5), (40, 64), (7, 333), (2, 5000)])
+def test_gradient_by_differences(B, n, d):
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    x, gy = (torch.randn(n, d, device="cuda", generator=gen) for _ in range(2))
+    w, b = params(d, torch.float32, gen)
+    _, mean, rstd = B.layer_norm(x, w, b)
+    grads = B.layer_norm_grad(gy, x, mean, rstd, w)
+    for k, (grad, where) in enumerate(zip(grads, (x, w, b))):
+        v = torch.randn(where.shape, device="cuda", generator=gen, dtype=torch.float64)
+        h = 1e-5
+
+        def loss(t):
+            moved = [p.double() + t * v if k == j else p.double() for j, p in enumerate((x, w, b))]
+            return (forward64(*moved, 1e-5)[0] * gy.double()).sum()
+
+        slope = ((loss(h) - loss(-h)) / (2 * h)).item()
+        # the differences' own error is about h^2 of the third derivative and 1e-16 / h of the sum; the gradient's elements have a few dozen roundings
+        size = (grad.double().abs() * v.abs()).sum().item() + (gy.double().abs().sum() * 1e-6).item()
+        assert abs((grad.double() * v).sum().item() - slope) <= (d + n + 40) * EPS * size + 1e-8 * gy.double().abs().sum().item()
+
+
+def test_views(B):
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    for dtype in TYPES:
+        wide, other = (torch.randn(300, 75, device="cuda", generator=gen).to(dtype) for _ in range(2))
+        for cut in (lambda t: t[:, 2:70], lambda t: t[::3, 1:9], lambda t: t[4:5].expand(300, 75), lambda t: t[:, 74:], lambda t: t[1:], lambda t: t[:, :64]):
+            x, gy = cut(wide), cut(other)
+            w, b = params(x.shape[1] + 1, torch.float32, gen)
+            w, b = w[1:], b[1:]
+            out = B.layer_norm(x, w, b)
+            check_forward(out, x, w, b, 1e-5)
+            check_grad(B.layer_norm_grad(gy, x, out[1], out[2], w), gy, x, out[1], out[2], w)
+
+
+def test_rows_without_spread_and_of_what_is_no_number(B):
+    for d in (1, 5, 64, 300, 5000):
+        x = torch.full((4, d), 3.25, device="cuda")
+        x[1] = 0
+        x[2] = 1e30                                        # far beyond where squares are finite: of the deviations, which are 0
+        w, b = torch.full((d,), 2.0, device="cuda"), torch.full((d,), -1.5, device="cuda")
+        y, mean, rstd = B.layer_norm(x, w, b)
+        assert torch.equal(y, torch.full_like(y, -1.5)) and torch.equal(mean, x[:, 0])
+        assert bool(((rstd.double() - 1e-5 ** -0.5).abs() <= 8 * EPS * 1e-5 ** -0.5).all())
+        x = torch.randn(6, d, device="cuda")
+        clean = B.layer_norm(x, w, b)
+        x[1, 0], x[3, d - 1], x[4, 0] = float("nan"), float("inf"), float("-inf")
+        y, mean, rstd = B.layer_norm(x, w, b)
+        for got, want in zip((y, mean, rstd), clean):
+            assert torch.equal(got[[0, 2, 5]], want[[0, 2, 5]])                    # other rows do not see it
+        assert bool(torch.isnan(y[[1, 3, 4]]).all())
+        gy = torch.randn(6, d, device="cuda")
+        gx = B.layer_norm_grad(gy, x, mean, rstd, w)[0]
+        assert bool(torch.isfinite(gx[[0, 2, 5]]).all()) and bool(torch.isnan(gx[[1, 3, 4]]).all())
+    # large offsets: the deviations are taken from the mean before they are squared
+    x = 1000.0 + torch.randn(50, 256, device="cuda")
+    check_forward(B.layer_norm(x), x, None, None, 1e-5)
+
+
+def test_nothing(B):
+    x = torch.zeros(0, 12, device="cuda")
+    y, mean, rstd = B.layer_norm(x)
+    assert y.shape == (0, 12) and mean.shape == (0,)
+    gx, gw, gb = B.layer_norm_grad(x, x, mean, rstd)
+    assert gx.shape == (0, 12) and not bool(gw.any()) and not bool(gb.any())
+
+
+def test_past_32_bits(B):
+    n, d = 1100000, 2000                                   # 2.2e9 elements
+    x = torch.empty(n, d, device="cuda", dtype=torch.bfloat16)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    ends = [0, 1, n // 2, n - 2, n - 1]
+    x.zero_()
+    for i in ends:
+        x[i] = torch.randn(d, device="cuda", generator=gen).bfloat16()
+    y, mean, rstd = B.layer_norm(x)
+    check_forward((y[ends], mean[ends], rstd[ends]), x[ends], None, None, 1e-5)
+    del y
+    gx, gw, gb = B.layer_norm_grad(x, x, mean, rstd)
+    check_grad((gx[ends], None, None), x[ends], x[ends], mean[ends], rstd[ends], None)
+    check_grad((gx[ends], gw, gb), x[ends], x[ends], mean[ends], rstd[ends], None)                       # all other rows are zero
+
+
+def test_on_another_stream_and_captured(B):
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    for n, d in ((7, 40), (5000, 64), (300, 5000)):
+        x, gy = (torch.randn(n, d, device="cuda", generator=gen) for _ in range(2))
+        w, b = params(d, torch.float32, gen)
+
+        def both():
+            out = B.layer_norm(x, w, b)
+            return *out, *B.layer_norm_grad(gy, x, out[1], out[2], w)
+
+        want = both()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            got = both()
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = both()
+        for _ in range(4):
+            x.copy_(torch.randn(n, d, device="cuda", generator=gen))
+            gy.copy_(torch.randn(n, d, device="cuda", generator=gen))
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(p, q) for p, q in zip(got, both()))
+            torch.cuda.synchronize()
+
+
+def test_refusals(B):
+    x, w = torch.randn(6, 8, device="cuda"), torch.ones(8, device="cuda")
+    y, mean, rstd = B.layer_norm(x, w)
+    for call in (lambda: B.layer_norm(x.cpu()), lambda: B.layer_norm(x.double()), lambda: B.layer_norm(x.t()), lambda: B.layer_norm(x, w[:7]), lambda: B.layer_norm(x, w.half()),
+                 lambda: B.layer_norm(x.half(), w.half(), w), lambda: B.layer_norm(x, w.cpu()), lambda: B.layer_norm(x[0]), lambda: B.layer_norm(x, torch.ones(16, device="cuda")[::2]),
+                 lambda: B.layer_norm_grad(x[:5], x, mean, rstd), lambda: B.layer_norm_grad(x.half(), x, mean, rstd), lambda: B.layer_norm_grad(x, x, mean[:5], rstd),
+                 lambda: B.layer_norm_grad(x, x, mean, rstd.double()), lambda: B.layer_norm_grad(x, x, mean, rstd, w[None])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: B.layer_norm(x[:, :0]), lambda: B.layer_norm(x, eps=-1.0), lambda: B.layer_norm(x, eps=float("nan"))):
+        with pytest.raises(B.HagError) as err:
+            call()
+        assert err.value.code == B.HAG_EINVAL
