@@ -21,4 +21,67 @@ static inline int id_switch(hag_dtype_t t, F f) {
     return t == HAG_I64 ? f(int64_t()) : f(int32_t());
 }
 
+// 16 bytes of a row: memory operations of that width at any address that suits one element, which gfx950's global loads and stores take.
+template <typename T>
+constexpr int kVec = 16 / (int)sizeof(T);
+template <typename T>
+struct VecOf {
+    typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+};
+
+// p[0 .. kVec) as it comes from memory.  Where not all of it is memory of the matrix (`readable`), the first `have` elements, the others 0.
+template <typename T>
+__device__ __forceinline__ typename VecOf<T>::type load_vec(const T *p, bool readable, int have) {
+    typename VecOf<T>::type raw = {};
+    if (readable) {
+        raw = *reinterpret_cast<const typename VecOf<T>::type *>(p);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kVec<T>; ++e)
+            if (e < have) raw[e] = p[e];
+    }
+    return raw;
+}
+template <typename T>
+__device__ __forceinline__ typename VecOf<T>::type load_vec(const T *p) { return *reinterpret_cast<const typename VecOf<T>::type *>(p); }
+
+// p[0 .. min(have, kVec)) = v, each rounded once
+template <typename T>
+__device__ __forceinline__ void store_vec(T *p, int have, const float (&v)[kVec<T>]) {
+    if (have >= kVec<T>) {
+        typename VecOf<T>::type raw;
+#pragma unroll
+        for (int e = 0; e < kVec<T>; ++e) raw[e] = (T)v[e];
+        *reinterpret_cast<typename VecOf<T>::type *>(p) = raw;
+    } else {
+#pragma unroll
+        for (int e = 0; e < kVec<T>; ++e)
+            if (e < have) p[e] = (T)v[e];
+    }
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_move(float v) {
+    return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+typedef unsigned elem_u2_t __attribute__((ext_vector_type(2)));
+
+// Sum over groups of W adjacent lanes (a power of two), in every lane of the group: moves within a row of 16 lanes, then swaps of rows and of halves.
+template <int W>
+__device__ __forceinline__ float lanes_sum(float v) {
+    if (W > 1) v += dpp_move<0xB1>(v);                     // lane ^ 1
+    if (W > 2) v += dpp_move<0x4E>(v);                     // lane ^ 2
+    if (W > 4) v += dpp_move<0x141>(v);                    // the other four of eight
+    if (W > 8) v += dpp_move<0x140>(v);                    // the other eight of sixteen
+    if (W > 16) {
+        const elem_u2_t s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s.x) + __uint_as_float(s.y);
+    }
+    if (W > 32) {
+        const elem_u2_t s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s.x) + __uint_as_float(s.y);
+    }
+    return v;
+}
+
 }  // namespace hag

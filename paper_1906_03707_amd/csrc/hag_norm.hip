@@ -1,104 +1,462 @@
 // Layer norm over the rows of a matrix, and its backward pass.
 //   m = mean of x over a row, r = 1 / sqrt(mean of (x - m)^2 + eps), xh = (x - m) r, y = xh w + b
 //   u = g_y w:  g_x = r (u - mean(u) - xh mean(u xh)),  g_w = sum over rows of g_y xh,  g_b = sum over rows of g_y
+// A row is read once and stays in registers: LPR adjacent lanes hold K vectors of 16 bytes each (lane l vectors l, l + LPR, ...), sums over a row are moves
+// between those lanes.  Statistics in fp32: the mean of the differences from the row's first element (rows of one value, however large, then have that
+// mean and no deviation), the variance of the deviations from the mean.  Rows of more than 1024 columns take a workgroup, of more than 8192 are read again for every sum.
 #include "hag_elem.hpp"
 
 namespace hag {
 
-__device__ __forceinline__ float block_sum(float v, float *lds) {
+struct NormArgs {
+    const void *x, *gy;
+    int64_t x_stride, gy_stride, n;
+    int64_t x_extent, gy_extent;     // elements from the first of the matrix to the end of its last row: what may be read
+    int32_t d, param32;              // param32: weight and bias are fp32, else they have the type of x
+    const void *weight, *bias;       // or NULL
+    float eps, inv_d;
+    void *out;                       // y or g_x, contiguous
+    const float *mean_in, *rstd_in;
+    float *mean, *rstd;              // or NULL
+    float *partial;                  // g_w and g_b of every workgroup [groups, 2, d]; NULL: not wanted, or one workgroup does it all
+    void *g_w, *g_b;                 // for one workgroup
+};
+
+// weight or bias of the columns of a vector; `otherwise` where there is none
+template <typename T, bool TAIL>
+__device__ __forceinline__ void load_params(const void *p, int param32, int col, int d, float otherwise, float (&v)[kVec<T>]) {
 #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) v += __shfl_xor(v, off);
+    for (int e = 0; e < kVec<T>; ++e) v[e] = otherwise;
+    if (!p || col >= d) return;
+    if (!param32) {
+        const typename VecOf<T>::type raw = load_vec((const T *)p + col, !TAIL || col + kVec<T> <= d, d - col);
+#pragma unroll
+        for (int e = 0; e < kVec<T>; ++e) v[e] = (float)raw[e];
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < kVec<T>; q += 4) {
+        const typename VecOf<float>::type raw = load_vec((const float *)p + col + q, !TAIL || col + q + 4 <= d, d - col - q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[q + e] = raw[e];
+    }
+}
+
+// Columns col .. col + kVec of the row at element `at`; lanes beyond the row's end get its first ones, so that no load waits for a condition.  TAIL: d is no multiple
+// of the vector, a row's last vector brings elements of the next row along, and at the end of the matrix is read element by element.
+template <typename T, bool TAIL>
+__device__ __forceinline__ typename VecOf<T>::type load_columns(const T *base, int64_t at, int col, int d, int64_t extent) {
+    const T *p = base + at + (col < d ? col : 0);
+    return TAIL ? load_vec(p, p - base + kVec<T> <= extent, d - col) : load_vec(p);
+}
+
+// Sums over a row, in all of its lanes.  Rows of up to 64 lanes: moves between lanes; longer ones: the workgroup, through LDS (two halves, used in turn, so that one barrier
+// a sum is enough).
+template <int LPR>
+__device__ __forceinline__ float2 row_sums(float2 v, float2 (*lds)[16], int &turn) {
+    v.x = lanes_sum<(LPR <= kWave ? LPR : kWave)>(v.x);
+    v.y = lanes_sum<(LPR <= kWave ? LPR : kWave)>(v.y);
+    if (LPR <= kWave) return v;
+    if (threadIdx.x % kWave == 0) lds[turn][threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < LPR / kWave; ++w) {
+        v.x += lds[turn][w].x;
+        v.y += lds[turn][w].y;
+    }
+    turn ^= 1;
+    return v;
+}
+
+// Threads of a workgroup whose rows have LPR lanes (backward: twice as many where rows have a wavefront or less, so that there are half as many partial sums), and the rows
+// that a wavefront (or the workgroup) takes side by side.
+template <int LPR>
+constexpr int kNormBlock = LPR <= kWave ? kBlock : LPR;
+template <int LPR>
+constexpr int kGradBlock = LPR <= kWave ? 2 * kBlock : LPR;
+template <int LPR>
+constexpr int kSide = LPR <= kWave ? kWave / LPR : 1;
+
+// Bound by reading x and writing y.  Every lane requests about four vectors before it needs one: R rows one after the other where a row has one or two vectors per lane.
+template <typename T, int LPR, int K, int R, bool TAIL>
+__global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
+    __shared__ float2 lds[2][16];
+    typedef typename VecOf<T>::type Raw;
+    constexpr int V = kVec<T>, kTaker = LPR <= kWave ? kWave : LPR;
+    const int l = threadIdx.x % LPR;
+    const int64_t row0 = ((int64_t)blockIdx.x * (kNormBlock<LPR> / kTaker) + threadIdx.x / kTaker) * (kSide<LPR> * R) + threadIdx.x % kTaker / LPR;
+    const T *x = (const T *)a.x;
+    Raw raw[R][K];
+    float first[R], m[R], r[R];
+    int turn = 0;
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        const int64_t at = min(row0 + t * kSide<LPR>, a.n - 1) * a.x_stride;       // (rows beyond the last one: that one again, not stored)
+        first[t] = (float)x[at];
+#pragma unroll
+        for (int k = 0; k < K; ++k) raw[t][k] = load_columns<T, TAIL>(x, at, (l + LPR * k) * V, a.d, a.x_extent);
+    }
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int col = (l + LPR * k) * V;
+            float part = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) part += !TAIL || col + e < a.d ? (float)raw[t][k][e] - first[t] : 0.f;
+            s += col < a.d ? part : 0.f;
+        }
+        m[t] = first[t] + row_sums<LPR>(make_float2(s, 0.f), lds, turn).x * a.inv_d;
+        s = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int col = (l + LPR * k) * V;
+            float part = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float v = (float)raw[t][k][e] - m[t];
+                part += !TAIL || col + e < a.d ? v * v : 0.f;
+            }
+            s += col < a.d ? part : 0.f;
+        }
+        r[t] = rsqrtf(row_sums<LPR>(make_float2(s, 0.f), lds, turn).x * a.inv_d + a.eps);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int col = (l + LPR * k) * V;
+        if (col >= a.d) continue;
+        float w[V], b[V];
+        load_params<T, TAIL>(a.weight, a.param32, col, a.d, 1.f, w);
+        load_params<T, TAIL>(a.bias, a.param32, col, a.d, 0.f, b);
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+            const int64_t row = row0 + t * kSide<LPR>;
+            if (row >= a.n) continue;
+            float v[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = ((float)raw[t][k][e] - m[t]) * r[t] * w[e] + b[e];
+            store_vec((T *)a.out + row * a.d + col, TAIL ? a.d - col : V, v);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        const int64_t row = row0 + t * kSide<LPR>;
+        if (l == 0 && row < a.n) {
+            if (a.mean) a.mean[row] = m[t];
+            if (a.rstd) a.rstd[row] = r[t];
+        }
+    }
+}
+
+// Bound by reading x and g_y and writing g_x.  Workgroups take rows in turn, keep the sums of their columns for g_w and g_b in registers, and leave them in `partial`, one
+// row of 2 d for each workgroup, added up in a fixed order by norm_reduce_kernel.  The next rows are requested before the present ones are worked on.
+template <typename T, int LPR, int K, int R, bool TAIL>
+__global__ __launch_bounds__(kGradBlock<LPR>) void norm_grad_kernel(NormArgs a) {
+    extern __shared__ float sums[];                        // [wavefronts][2][LPR * K * V], rows of up to 64 lanes
+    __shared__ float2 lds[2][16];
+    typedef typename VecOf<T>::type Raw;
+    constexpr int V = kVec<T>, kTaker = LPR <= kWave ? kWave : LPR, kTakers = kGradBlock<LPR> / kTaker;   // what takes a set of rows: a wavefront, or the workgroup
+    const int l = threadIdx.x % LPR, side = threadIdx.x % kTaker / LPR;
+    const T *x = (const T *)a.x, *gy = (const T *)a.gy;
+    int turn = 0;
+    float w[K][V], gw[K][V], gb[K][V];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        load_params<T, TAIL>(a.weight, a.param32, (l + LPR * k) * V, a.d, 1.f, w[k]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) gw[k][e] = gb[k][e] = 0.f;
+    }
+    const int64_t sets = (a.n + kSide<LPR> * R - 1) / (kSide<LPR> * R), step = (int64_t)gridDim.x * kTakers;
+    struct Rows {
+        Raw x[R][K], g[R][K];
+        float m[R], r[R];
+    };
+    auto request = [&](int64_t set, Rows &q) {
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+            const int64_t row = min((set * R + t) * kSide<LPR> + side, a.n - 1);
+            q.m[t] = a.mean_in[row];
+            q.r[t] = a.rstd_in[row];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                q.x[t][k] = load_columns<T, TAIL>(x, row * a.x_stride, (l + LPR * k) * V, a.d, a.x_extent);
+                q.g[t][k] = load_columns<T, TAIL>(gy, row * a.gy_stride, (l + LPR * k) * V, a.d, a.gy_extent);
+            }
+        }
+    };
+    auto work = [&](int64_t set, const Rows &q) {
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+            const int64_t row = (set * R + t) * kSide<LPR> + side;
+            const bool here = row < a.n;
+            float2 s = make_float2(0.f, 0.f);
+            float xh[K][V], u[K][V];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int col = (l + LPR * k) * V;
+                float2 part = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const bool in = here && (!TAIL || col + e < a.d);
+                    const float g = in ? (float)q.g[t][k][e] : 0.f;
+                    xh[k][e] = in ? ((float)q.x[t][k][e] - q.m[t]) * q.r[t] : 0.f;
+                    u[k][e] = g * w[k][e];
+                    gw[k][e] += g * xh[k][e];              // (columns beyond the row's end: not read)
+                    gb[k][e] += g;
+                    part.x += u[k][e];
+                    part.y += u[k][e] * xh[k][e];
+                }
+                s.x += col < a.d ? part.x : 0.f;
+                s.y += col < a.d ? part.y : 0.f;
+            }
+            s = row_sums<LPR>(s, lds, turn);
+            s.x *= a.inv_d;
+            s.y *= a.inv_d;
+            if (!here) continue;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int col = (l + LPR * k) * V;
+                if (col >= a.d) continue;
+#pragma unroll
+                for (int e = 0; e < V; ++e) u[k][e] = q.r[t] * (u[k][e] - s.x - xh[k][e] * s.y);
+                store_vec((T *)a.out + row * a.d + col, TAIL ? a.d - col : V, u[k]);
+            }
+        }
+    };
+    int64_t set = (int64_t)blockIdx.x * kTakers + threadIdx.x / kTaker;
+    if (set < sets) {
+        Rows q;
+        request(set, q);
+        for (; set < sets; set += step) {
+            Rows next = q;
+            if (set + step < sets) request(set + step, next);
+            work(set, q);
+            q = next;
+        }
+    }
+    if (!a.partial && !a.g_w && !a.g_b) return;
+    auto leave = [&](int c, float w_sum, float b_sum) {
+        if (a.partial) {
+            a.partial[(int64_t)blockIdx.x * 2 * a.d + c] = w_sum;
+            a.partial[((int64_t)blockIdx.x * 2 + 1) * a.d + c] = b_sum;
+        } else if (a.param32) {
+            if (a.g_w) ((float *)a.g_w)[c] = w_sum;
+            if (a.g_b) ((float *)a.g_b)[c] = b_sum;
+        } else {
+            if (a.g_w) ((T *)a.g_w)[c] = (T)w_sum;
+            if (a.g_b) ((T *)a.g_b)[c] = (T)b_sum;
+        }
+    };
+    if (LPR > kWave) {                                     // every column has one lane
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if ((l + LPR * k) * V + e < a.d) leave((l + LPR * k) * V + e, gw[k][e], gb[k][e]);
+        return;
+    }
+    // lanes that hold the same columns, then the wavefronts in their order
+    constexpr int kWidth = LPR * K * V;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+#pragma unroll
+            for (int off = LPR; off < kWave; off <<= 1) {
+                gw[k][e] += __shfl_xor(gw[k][e], off);
+                gb[k][e] += __shfl_xor(gb[k][e], off);
+            }
+    if (threadIdx.x % kWave < LPR) {
+        float *mine = sums + threadIdx.x / kWave * (2 * kWidth);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                mine[(l + LPR * k) * V + e] = gw[k][e];
+                mine[kWidth + (l + LPR * k) * V + e] = gb[k][e];
+            }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.d; c += kGradBlock<LPR>) {
+        float w_sum = 0.f, b_sum = 0.f;
+#pragma unroll
+        for (int wave = 0; wave < kTakers; ++wave) {
+            w_sum += sums[wave * 2 * kWidth + c];
+            b_sum += sums[(wave * 2 + 1) * kWidth + c];
+        }
+        leave(c, w_sum, b_sum);
+    }
+}
+
+// g_w and g_b: 16 columns per workgroup, 64 threads for each, which take every 64th row of `partial`, then those in a fixed order
+template <typename P>
+__global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *__restrict__ partial, int32_t groups, int32_t d, P *__restrict__ g_w, P *__restrict__ g_b) {
+    __shared__ float part[64][17];
+    const int o = threadIdx.x & 15, p = threadIdx.x >> 4, i = blockIdx.x * 16 + o;
+    float sum = 0.f;
+    if (i < 2 * d) {
+#pragma unroll 8
+        for (int g = p; g < groups; g += 64) sum += partial[(int64_t)g * 2 * d + i];
+    }
+    part[p][o] = sum;
+    __syncthreads();
+    for (int half = 32; half > 0; half >>= 1) {
+        if (p < half) part[p][o] += part[p + half][o];
+        __syncthreads();
+    }
+    if (p != 0 || i >= 2 * d) return;
+    if (i < d) {
+        if (g_w) g_w[i] = (P)part[0][o];
+    } else if (g_b) {
+        g_b[i - d] = (P)part[0][o];
+    }
+}
+
+// Rows that registers do not hold: a workgroup of 1024 reads its row again for every sum.
+constexpr int kWide = 1024;
+__device__ __forceinline__ float wide_sum(float v, float *lds) {
+    v = lanes_sum<kWave>(v);
     __syncthreads();
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
     __syncthreads();
     v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kBlock / kWave; ++w) v += lds[w];
+    for (int w = 0; w < kWide / kWave; ++w) v += lds[w];
     return v;
 }
 
-template <typename T, typename P>
-__global__ __launch_bounds__(kBlock) void norm_kernel(const T *__restrict__ x, int64_t stride, int32_t d, const P *__restrict__ w, const P *__restrict__ b, float eps,
-                                                      T *__restrict__ y, float *__restrict__ mean, float *__restrict__ rstd) {
-    __shared__ float lds[kBlock / kWave];
+__device__ __forceinline__ float param(const void *p, int param32, float, int c) { return ((const float *)p)[c]; }
+template <typename T>
+__device__ __forceinline__ float param(const void *p, int param32, T, int c) { return param32 ? ((const float *)p)[c] : (float)((const T *)p)[c]; }
+
+template <typename T>
+__global__ __launch_bounds__(kWide) void norm_wide_kernel(NormArgs a) {
+    __shared__ float lds[kWide / kWave];
     const int64_t row = blockIdx.x;
-    const T *p = x + row * stride;
-    // the mean is taken of the differences from the row's first element: rows of one value, however large, then have that mean and no deviation
+    const T *p = (const T *)a.x + row * a.x_stride;
     const float first = (float)p[0];
     float s = 0.f;
-    for (int c = threadIdx.x; c < d; c += kBlock) s += (float)p[c] - first;
-    const float m = first + block_sum(s, lds) / d;
+    for (int c = threadIdx.x; c < a.d; c += kWide) s += (float)p[c] - first;
+    const float m = first + wide_sum(s, lds) * a.inv_d;
     s = 0.f;
-    for (int c = threadIdx.x; c < d; c += kBlock) { const float v = (float)p[c] - m; s += v * v; }
-    const float r = 1.f / sqrtf(block_sum(s, lds) / d + eps);
-    for (int c = threadIdx.x; c < d; c += kBlock) {
+    for (int c = threadIdx.x; c < a.d; c += kWide) { const float v = (float)p[c] - m; s += v * v; }
+    const float r = rsqrtf(wide_sum(s, lds) * a.inv_d + a.eps);
+    for (int c = threadIdx.x; c < a.d; c += kWide) {
         const float xh = ((float)p[c] - m) * r;
-        y[row * d + c] = (T)(xh * (w ? (float)w[c] : 1.f) + (b ? (float)b[c] : 0.f));
+        ((T *)a.out)[row * a.d + c] = (T)(xh * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f) + (a.bias ? param(a.bias, a.param32, T(), c) : 0.f));
     }
     if (threadIdx.x == 0) {
-        if (mean) mean[row] = m;
-        if (rstd) rstd[row] = r;
+        if (a.mean) a.mean[row] = m;
+        if (a.rstd) a.rstd[row] = r;
     }
 }
 
-template <typename T, typename P>
-__global__ __launch_bounds__(kBlock) void norm_grad_kernel(const T *__restrict__ gy, int64_t gy_stride, const T *__restrict__ x, int64_t stride, int32_t d,
-                                                           const P *__restrict__ w, const float *__restrict__ mean, const float *__restrict__ rstd, T *__restrict__ gx) {
-    __shared__ float lds[kBlock / kWave];
+template <typename T>
+__global__ __launch_bounds__(kWide) void norm_grad_wide_kernel(NormArgs a) {
+    __shared__ float lds[kWide / kWave];
     const int64_t row = blockIdx.x;
-    const T *p = x + row * stride, *g = gy + row * gy_stride;
-    const float m = mean[row], r = rstd[row];
+    const T *p = (const T *)a.x + row * a.x_stride, *g = (const T *)a.gy + row * a.gy_stride;
+    const float m = a.mean_in[row], r = a.rstd_in[row];
     float s1 = 0.f, s2 = 0.f;
-    for (int c = threadIdx.x; c < d; c += kBlock) {
-        const float u = (float)g[c] * (w ? (float)w[c] : 1.f);
+    for (int c = threadIdx.x; c < a.d; c += kWide) {
+        const float u = (float)g[c] * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f);
         s1 += u;
         s2 += u * (((float)p[c] - m) * r);
     }
-    s1 = block_sum(s1, lds) / d;
-    s2 = block_sum(s2, lds) / d;
-    for (int c = threadIdx.x; c < d; c += kBlock) {
-        const float u = (float)g[c] * (w ? (float)w[c] : 1.f);
-        gx[row * d + c] = (T)(r * (u - s1 - ((float)p[c] - m) * r * s2));
+    s1 = wide_sum(s1, lds) * a.inv_d;
+    s2 = wide_sum(s2, lds) * a.inv_d;
+    for (int c = threadIdx.x; c < a.d; c += kWide) {
+        const float u = (float)g[c] * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f);
+        ((T *)a.out)[row * a.d + c] = (T)(r * (u - s1 - ((float)p[c] - m) * r * s2));
     }
 }
 
-// partial[slice] = the sums of a slice of the rows, [2, d]: g_w, g_b
+// partial[slice] = the sums of a slice of the rows, 64 columns per workgroup
 template <typename T>
-__global__ __launch_bounds__(kBlock) void norm_sums_kernel(const T *__restrict__ gy, int64_t gy_stride, const T *__restrict__ x, int64_t stride, int64_t n, int32_t d,
-                                                           const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ partial) {
+__global__ __launch_bounds__(kBlock) void norm_wide_sums_kernel(NormArgs a) {
     __shared__ float lds[kBlock / kWave][2][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
     float gw = 0.f, gb = 0.f;
-    if (c < d) {
-        for (int64_t row = (int64_t)blockIdx.y * (kBlock / kWave) + wave; row < n; row += (int64_t)gridDim.y * (kBlock / kWave)) {
-            const float g = (float)gy[row * gy_stride + c];
-            gw += g * (((float)x[row * stride + c] - mean[row]) * rstd[row]);
+    if (c < a.d) {
+        for (int64_t row = (int64_t)blockIdx.y * (kBlock / kWave) + wave; row < a.n; row += (int64_t)gridDim.y * (kBlock / kWave)) {
+            const float g = (float)((const T *)a.gy)[row * a.gy_stride + c];
+            gw += g * (((float)((const T *)a.x)[row * a.x_stride + c] - a.mean_in[row]) * a.rstd_in[row]);
             gb += g;
         }
     }
     lds[wave][0][lane] = gw;
     lds[wave][1][lane] = gb;
     __syncthreads();
-    if (wave > 0 || c >= d) return;
+    if (wave > 0 || c >= a.d) return;
     for (int v = 1; v < kBlock / kWave; ++v) { gw += lds[v][0][lane]; gb += lds[v][1][lane]; }
-    partial[((int64_t)blockIdx.y * 2) * d + c] = gw;
-    partial[((int64_t)blockIdx.y * 2 + 1) * d + c] = gb;
+    a.partial[((int64_t)blockIdx.y * 2) * a.d + c] = gw;
+    a.partial[((int64_t)blockIdx.y * 2 + 1) * a.d + c] = gb;
 }
 
-template <typename P>
-__global__ __launch_bounds__(kBlock) void norm_reduce_kernel(const float *__restrict__ partial, int32_t slices, int32_t d, P *__restrict__ g_w, P *__restrict__ g_b) {
-    const int i = blockIdx.x * kBlock + threadIdx.x;
-    if (i >= 2 * d) return;
-    float sum = 0.f;
-    for (int s = 0; s < slices; ++s) sum += partial[(int64_t)s * 2 * d + i];
-    if (i < d) {
-        if (g_w) g_w[i] = (P)sum;
-    } else if (g_b) {
-        g_b[i - d] = (P)sum;
+// How a row is held: lanes per row, vectors per lane (0: not in registers).  A lane has at most 16 columns, whose gradients of weight and bias take as many registers each.
+struct NormShape { int lpr, k; };
+static NormShape norm_shape(int64_t d, int vec) {
+    const int64_t nv = (d + vec - 1) / vec;
+    int lpr = 2;
+    while (lpr < kWave && lpr < nv) lpr *= 2;
+    if (nv <= (16 / vec) * kWave) return {lpr, (int)((nv + kWave - 1) / kWave)};
+    if (nv <= 256) return {256, 1};
+    return nv <= 512 ? NormShape{256, 2} : nv <= 1024 ? NormShape{1024, 1} : nv <= 2048 && vec == 4 ? NormShape{1024, 2} : NormShape{1024, 0};
+}
+
+typedef void (*norm_kernel_t)(NormArgs);
+template <typename T, template <int, int> class F>
+static norm_kernel_t norm_pick(NormShape s) {
+    switch (s.lpr) {
+    case 2: return F<2, 1>::kernel;
+    case 4: return F<4, 1>::kernel;
+    case 8: return F<8, 1>::kernel;
+    case 16: return F<16, 1>::kernel;
+    case 32: return F<32, 1>::kernel;
+    case 64:
+        if constexpr (kVec<T> == 4) {
+            if (s.k > 2) return s.k == 3 ? (norm_kernel_t)F<64, 3>::kernel : (norm_kernel_t)F<64, 4>::kernel;
+        }
+        return s.k == 1 ? (norm_kernel_t)F<64, 1>::kernel : (norm_kernel_t)F<64, 2>::kernel;
+    case 256:
+        if constexpr (kVec<T> == 8) {
+            if (s.k == 1) return F<256, 1>::kernel;
+        }
+        return F<256, 2>::kernel;
+    default:
+        if constexpr (kVec<T> == 4) {
+            if (s.k == 2) return F<1024, 2>::kernel;
+        }
+        return F<1024, 1>::kernel;
     }
 }
+// Rows one after the other that a lane requests at once.
+constexpr int norm_rows(int lpr, int k) { return lpr > kWave ? 1 : k == 1 ? 4 : k == 2 ? 2 : 1; }
+constexpr int norm_grad_rows(int lpr, int k) { return lpr <= kWave && k == 1 ? 2 : 1; }
+// Threads of a workgroup, and the rows that it takes side by side.
+static int norm_block(NormShape s, bool backward) { return s.lpr <= kWave ? (backward ? 2 * kBlock : kBlock) : s.lpr; }
+static int64_t norm_side(NormShape s, bool backward) { return norm_block(s, backward) / s.lpr; }
+template <typename T, bool TAIL>
+struct Forward {
+    template <int LPR, int K>
+    struct Of { static constexpr auto kernel = norm_kernel<T, LPR, K, norm_rows(LPR, K), TAIL>; };
+};
+template <typename T, bool TAIL>
+struct Backward {
+    template <int LPR, int K>
+    struct Of { static constexpr auto kernel = norm_grad_kernel<T, LPR, K, norm_grad_rows(LPR, K), TAIL>; };
+};
 
-constexpr int kNormSlices = 128;
+// Workgroups of a backward pass.  One for each of the 256 compute units, so that few partial sums are written and read again; two where rows are shorter than a wavefront and those
+// sums are small (370000 x 64 fp32: 52.9 us with 256, 51.9 with 512; 65536 x 512 79.9 and 81.5, 16384 x 1024 38.8 and 41.2).
+constexpr int64_t kNormSlices = 128;
+static int64_t norm_grad_groups(int64_t n, NormShape s) {
+    if (s.k == 0) return kNormSlices;
+    const int64_t rows = s.lpr <= kWave ? norm_side(s, true) * norm_grad_rows(s.lpr, s.k) * 4 : 8;
+    return std::max<int64_t>(1, std::min<int64_t>((n + rows - 1) / rows, s.lpr < kWave ? 512 : 256));
+}
 
 }  // namespace hag
 
@@ -120,21 +478,39 @@ int hag_layer_norm(int64_t n, int64_t d, hag_dtype_t dtype, const void *x, int64
     if (!(eps >= 0.f)) { set_error("eps must not be negative"); return HAG_EINVAL; }
     if (n == 0) return HAG_OK;
     if (!x || !y) { set_error("NULL pointer"); return HAG_EINVAL; }
+    NormArgs a = {};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.n = n;
+    a.x_extent = (n - 1) * x_stride + d;
+    a.d = (int32_t)d;
+    a.param32 = param_dtype == HAG_F32;
+    a.weight = weight;
+    a.bias = bias;
+    a.eps = eps;
+    a.inv_d = 1.f / (float)d;
+    a.out = y;
+    a.mean = mean;
+    a.rstd = rstd;
     return elem_switch(dtype, [&](auto e) {
         using T = decltype(e);
-        auto launch = [&](auto p) {
-            using P = decltype(p);
-            hipLaunchKernelGGL((norm_kernel<T, P>), dim3((unsigned)n), dim3(kBlock), 0, (hipStream_t)stream, (const T *)x, x_stride, (int32_t)d, (const P *)weight, (const P *)bias, eps,
-                               (T *)y, mean, rstd);
-            HIP_TRY(hipGetLastError());
-            return (int)HAG_OK;
-        };
-        return param_dtype == dtype ? launch(T()) : launch(float());
+        const NormShape s = norm_shape(d, kVec<T>);
+        if (s.k == 0) {
+            hipLaunchKernelGGL(norm_wide_kernel<T>, dim3((unsigned)n), dim3(kWide), 0, (hipStream_t)stream, a);
+        } else {
+            const int64_t rows = norm_side(s, false) * norm_rows(s.lpr, s.k);
+            const norm_kernel_t kernel = d % kVec<T> ? norm_pick<T, Forward<T, true>::template Of>(s) : norm_pick<T, Forward<T, false>::template Of>(s);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((n + rows - 1) / rows)), dim3((unsigned)norm_block(s, false)), 0, (hipStream_t)stream, a);
+        }
+        HIP_TRY(hipGetLastError());
+        return (int)HAG_OK;
     });
 }
 
 size_t hag_layer_norm_grad_workspace_bytes(int64_t n, int64_t d) {
-    return norm_refusal(n, d, HAG_F32, HAG_F32) ? 0 : (size_t)kNormSlices * 2 * (size_t)d * sizeof(float);
+    if (norm_refusal(n, d, HAG_F32, HAG_F32)) return 0;
+    // the types of 16 bits take fewer lanes to a row and no more workgroups
+    return (size_t)std::max(norm_grad_groups(n, norm_shape(d, 4)), norm_grad_groups(n, norm_shape(d, 8))) * 2 * (size_t)d * sizeof(float);
 }
 
 int hag_layer_norm_grad(int64_t n, int64_t d, hag_dtype_t dtype, const void *g_y, int64_t g_y_stride, const void *x, int64_t x_stride, hag_dtype_t param_dtype, const void *weight,
@@ -144,27 +520,49 @@ int hag_layer_norm_grad(int64_t n, int64_t d, hag_dtype_t dtype, const void *g_y
     const bool params = g_weight || g_bias;
     if ((n > 0 && (!g_y || !x || !mean || !rstd || !g_x)) || (params && !workspace)) { set_error("NULL pointer"); return HAG_EINVAL; }
     if ((uintptr_t)workspace & 15) { set_error("workspace must be 16-byte aligned"); return HAG_EINVAL; }
+    if (n == 0 && !params) return HAG_OK;
     hipStream_t s = (hipStream_t)stream;
+    NormArgs a = {};
+    a.x = x;
+    a.gy = g_y;
+    a.x_stride = x_stride;
+    a.gy_stride = g_y_stride;
+    a.n = n;
+    a.x_extent = n > 0 ? (n - 1) * x_stride + d : 0;
+    a.gy_extent = n > 0 ? (n - 1) * g_y_stride + d : 0;
+    a.d = (int32_t)d;
+    a.param32 = param_dtype == HAG_F32;
+    a.weight = weight;
+    a.inv_d = 1.f / (float)d;
+    a.out = g_x;
+    a.mean_in = mean;
+    a.rstd_in = rstd;
     return elem_switch(dtype, [&](auto e) {
         using T = decltype(e);
-        auto launch = [&](auto p) {
-            using P = decltype(p);
-            if (n > 0) {
-                hipLaunchKernelGGL((norm_grad_kernel<T, P>), dim3((unsigned)n), dim3(kBlock), 0, s, (const T *)g_y, g_y_stride, (const T *)x, x_stride, (int32_t)d, (const P *)weight, mean,
-                                   rstd, (T *)g_x);
-                HIP_TRY(hipGetLastError());
-            }
-            if (params) {
-                hipLaunchKernelGGL(norm_sums_kernel<T>, dim3((unsigned)((d + kWave - 1) / kWave), kNormSlices), dim3(kBlock), 0, s, (const T *)g_y, g_y_stride, (const T *)x, x_stride, n,
-                                   (int32_t)d, mean, rstd, (float *)workspace);
-                HIP_TRY(hipGetLastError());
-                hipLaunchKernelGGL(norm_reduce_kernel<P>, dim3((unsigned)((2 * d + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, (const float *)workspace, kNormSlices, (int32_t)d,
-                                   (P *)g_weight, (P *)g_bias);
-                HIP_TRY(hipGetLastError());
-            }
-            return (int)HAG_OK;
-        };
-        return param_dtype == dtype ? launch(T()) : launch(float());
+        const NormShape shape = norm_shape(d, kVec<T>);
+        const int64_t groups = norm_grad_groups(n, shape);
+        if (groups > 1) {
+            a.partial = params ? (float *)workspace : nullptr;
+        } else {
+            a.g_w = g_weight;
+            a.g_b = g_bias;
+        }
+        if (shape.k == 0) {
+            if (n > 0) hipLaunchKernelGGL(norm_grad_wide_kernel<T>, dim3((unsigned)n), dim3(kWide), 0, s, a);
+            HIP_TRY(hipGetLastError());
+            if (params) hipLaunchKernelGGL(norm_wide_sums_kernel<T>, dim3((unsigned)((d + kWave - 1) / kWave), (unsigned)groups), dim3(kBlock), 0, s, a);
+        } else {
+            const size_t lds = shape.lpr <= kWave ? (size_t)(norm_block(shape, true) / kWave) * shape.lpr * shape.k * kVec<T> * 2 * sizeof(float) : 0;
+            const norm_kernel_t kernel = d % kVec<T> ? norm_pick<T, Backward<T, true>::template Of>(shape) : norm_pick<T, Backward<T, false>::template Of>(shape);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)norm_block(shape, true)), lds, s, a);
+        }
+        HIP_TRY(hipGetLastError());
+        if (!a.partial) return (int)HAG_OK;
+        const dim3 grid((unsigned)((2 * d + 15) / 16)), block(1024);
+        if (a.param32) hipLaunchKernelGGL(norm_reduce_kernel<float>, grid, block, 0, s, a.partial, (int32_t)groups, (int32_t)d, (float *)g_weight, (float *)g_bias);
+        else hipLaunchKernelGGL(norm_reduce_kernel<T>, grid, block, 0, s, a.partial, (int32_t)groups, (int32_t)d, (T *)g_weight, (T *)g_bias);
+        HIP_TRY(hipGetLastError());
+        return (int)HAG_OK;
     });
 }
 
