@@ -60,6 +60,30 @@ __device__ __forceinline__ void store_vec(T *p, int have, const float (&v)[kVec<
     }
 }
 
+// The same into a row of fp32, whatever the vector's length.
+template <typename O, int V>
+__device__ __forceinline__ void store_cols(O *p, int have, const float (&v)[V]) {
+    if constexpr (V == kVec<O>) {
+        store_vec(p, have, v);
+    } else {
+#pragma unroll
+        for (int q = 0; q < V; q += kVec<O>) {
+            float part[kVec<O>];
+#pragma unroll
+            for (int e = 0; e < kVec<O>; ++e) part[e] = v[q + e];
+            store_vec(p + q, have - q, part);
+        }
+    }
+}
+
+// Columns col .. col + kVec of the row at element `at` of a matrix whose last row ends at `extent`; lanes beyond the row's end get its first ones, so that no load waits for a
+// condition.  TAIL: d is no multiple of the vector, a row's last vector brings elements of the next row along, and at the end of the matrix is read element by element.
+template <typename T, bool TAIL>
+__device__ __forceinline__ typename VecOf<T>::type load_columns(const T *base, int64_t at, int col, int d, int64_t extent) {
+    const T *p = base + at + (col < d ? col : 0);
+    return TAIL ? load_vec(p, p - base + kVec<T> <= extent, d - col) : load_vec(p);
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp_move(float v) {
     return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));

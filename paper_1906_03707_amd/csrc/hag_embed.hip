@@ -1,40 +1,508 @@
 // Rows of a table looked up by id, and the gradient of the table.
 //   y[i] = scale * table[id[i]],   g_table[v] = scale * (sum over the i with id[i] = v of g_y[i])
 // An id equal to `padding` gives a row of zeros, one outside the table a row of NaN; neither sends a gradient.
+// The gradient sorts the tokens by id (stable, so that equal ids stay in their order and every sum has one fixed order), cuts the sorted list into equal pieces
+// whatever the ids are, and adds up runs of equal ids: a piece's inner runs are rows of g_table, runs that cross pieces are joined afterwards.
 #include "hag_elem.hpp"
 
 namespace hag {
 
-template <typename T, typename I>
-__global__ __launch_bounds__(kBlock) void embed_kernel(const T *__restrict__ table, int64_t stride, const I *__restrict__ ids, int64_t n, int64_t rows, int32_t d,
-                                                       int64_t padding, float scale, T *__restrict__ y) {
-    const int lane = threadIdx.x % kWave;
-    const int64_t i = (int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave;
-    if (i >= n) return;
-    const int64_t id = ids[i];
-    const bool named = id >= 0 && id < rows && id != padding;
-    for (int c = lane; c < d; c += kWave) y[i * d + c] = (T)(named ? scale * (float)table[id * stride + c] : id == padding ? 0.f : NAN);
+// ------------------------------------------------------------------------------------------------------------------ lookup
+
+struct EmbedArgs {
+    const void *table, *ids;
+    void *y;
+    int64_t stride, extent;          // of the table: elements to the next row, to the end of the last one
+    int64_t n, rows, padding;
+    int32_t d;
+    float scale;
+};
+
+// Bound by writing y (and by reading the table where it exceeds the caches).  LPR lanes move a row, 16 bytes each, four rows at a time: the ids first, then the rows they name.
+constexpr int kEmbedRows = 4;
+template <typename T, typename I, int LPR, bool TAIL>
+__global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
+    constexpr int V = kVec<T>, R = kEmbedRows;
+    const int l = threadIdx.x % LPR;
+    const int64_t row0 = ((int64_t)blockIdx.x * (kBlock / LPR) + threadIdx.x / kWave * (kWave / LPR)) * R + threadIdx.x % kWave / LPR;
+    const T *table = (const T *)a.table;
+    const I *ids = (const I *)a.ids;
+    int64_t id[R];
+    float other[R];                                        // what an id that names no row gives
+#pragma unroll
+    for (int t = 0; t < R; ++t) id[t] = ids[min(row0 + t * (kWave / LPR), a.n - 1)];
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        other[t] = id[t] == a.padding ? 0.f : NAN;
+        if (id[t] < 0 || id[t] >= a.rows || id[t] == a.padding) id[t] = -1;
+    }
+    for (int col = l * V; col < a.d; col += LPR * V) {
+        typename VecOf<T>::type raw[R] = {};
+        if (a.rows > 0) {
+#pragma unroll
+            for (int t = 0; t < R; ++t) raw[t] = load_columns<T, TAIL>(table, (id[t] < 0 ? 0 : id[t]) * a.stride, col, a.d, a.extent);
+        }
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+            const int64_t row = row0 + t * (kWave / LPR);
+            if (row >= a.n) continue;
+            float v[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = id[t] < 0 ? other[t] : a.scale * (float)raw[t][e];
+            store_vec((T *)a.y + row * a.d + col, TAIL ? a.d - col : V, v);
+        }
+    }
 }
 
-// One wavefront per row of the table looks through all ids and adds up the rows of g_y that name it, in their order.
-template <typename T, typename O, typename I>
-__global__ __launch_bounds__(kBlock) void embed_grad_kernel(const T *__restrict__ gy, int64_t stride, const I *__restrict__ ids, int64_t n, int64_t rows, int32_t d,
-                                                            int64_t padding, float scale, O *__restrict__ out) {
-    const int lane = threadIdx.x % kWave;
-    const int64_t v = (int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave;
-    if (v >= rows) return;
-    for (int c0 = 0; c0 < d; c0 += kWave) {
-        const int c = c0 + lane;
-        float sum = 0.f;
-        for (int64_t at = 0; at < n && v != padding; at += kWave) {
-            uint64_t hits = __ballot(at + lane < n && (int64_t)ids[at + lane] == v);
-            for (; hits; hits &= hits - 1) {
-                const int64_t i = at + __builtin_ctzll(hits);
-                if (c < d) sum += (float)gy[i * stride + c];
+// ------------------------------------------------------------------------------------------------------------------ order of the tokens
+
+// A token's key is its id, `rows` where it names no row: those come last and are left out.  Radix sort, low digits first, with stable passes of up to 10 bits:
+// counts per piece of the list, then every piece finds where each of its digits begins (the counts of smaller digits and of earlier pieces) and writes its tokens there.
+constexpr int kSortBlock = 512, kSortWaves = kSortBlock / kWave, kSortRounds = 8, kSortTile = kSortBlock * kSortRounds, kSortBits = 10, kSortPieces = 128;
+struct SortArgs {
+    const void *ids;                 // first pass: the tokens' ids
+    const uint32_t *keys, *tokens;   // later passes: what the one before wrote
+    uint32_t *keys_out, *tokens_out, *counts;
+    int64_t n, rows, padding, piece; // tokens of a piece, a multiple of kSortTile
+    int32_t pieces, shift, bits;
+};
+
+template <typename I>
+__device__ __forceinline__ uint32_t token_key(const I *ids, int64_t i, int64_t rows, int64_t padding) {
+    const int64_t id = ids[i];
+    return id >= 0 && id < rows && id != padding ? (uint32_t)id : (uint32_t)rows;
+}
+template <typename I, bool FIRST>
+__device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int64_t i) {
+    return FIRST ? token_key((const I *)a.ids, i, a.rows, a.padding) : a.keys[i];
+}
+
+// lanes whose digit is this lane's, among those of `active`
+__device__ __forceinline__ uint64_t equal_digits(uint32_t digit, int bits, uint64_t active) {
+    for (int b = 0; b < bits; ++b) {
+        const bool set = digit >> b & 1;
+        const uint64_t with = __ballot(set);
+        active &= set ? with : ~with;
+    }
+    return active;
+}
+
+template <typename I, bool FIRST>
+__global__ __launch_bounds__(kSortBlock) void sort_count_kernel(SortArgs a) {
+    __shared__ uint32_t count[1 << kSortBits];
+    const int digits = 1 << a.bits;
+    for (int c = threadIdx.x; c < digits; c += kSortBlock) count[c] = 0;
+    __syncthreads();
+    const int64_t begin = (int64_t)blockIdx.x * a.piece, end = min(begin + a.piece, a.n);
+    for (int64_t i = begin + threadIdx.x; i < end; i += kSortBlock) atomicAdd(&count[sort_key<I, FIRST>(a, i) >> a.shift & (digits - 1)], 1u);
+    __syncthreads();
+    for (int c = threadIdx.x; c < digits; c += kSortBlock) a.counts[(int64_t)blockIdx.x * digits + c] = count[c];
+}
+
+// Within a tile a wavefront takes 512 tokens in their order, 64 at a time; a token's place is where its digit begins, plus the tokens of that digit in earlier
+// wavefronts of the tile, in earlier rounds of its own, and in lower lanes.
+template <typename I, bool FIRST>
+__global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
+    __shared__ uint32_t count[kSortWaves][1 << kSortBits], base[1 << kSortBits], total[1 << kSortBits], wave_sum[kSortWaves];
+    const int digits = 1 << a.bits, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    for (int c = threadIdx.x; c < digits; c += kSortBlock) base[c] = total[c] = 0;
+    __syncthreads();
+    {
+        const int slices = max(1, kSortBlock >> a.bits);
+        for (int c = threadIdx.x; c < digits * slices; c += kSortBlock) {
+            const int digit = c & (digits - 1);
+            uint32_t all = 0, before = 0;
+#pragma unroll 16
+            for (int p = c >> a.bits; p < a.pieces; p += slices) {
+                const uint32_t v = a.counts[(int64_t)p * digits + digit];
+                all += v;
+                before += p < (int)blockIdx.x ? v : 0;
+            }
+            atomicAdd(&total[digit], all);
+            atomicAdd(&base[digit], before);
+        }
+    }
+    __syncthreads();
+    {   // base[digit] += tokens of smaller digits: two digits a thread, then lanes, then wavefronts
+        const int c = 2 * threadIdx.x;
+        const uint32_t t0 = c < digits ? total[c] : 0, t1 = c + 1 < digits ? total[c + 1] : 0;
+        uint32_t sum = t0 + t1;
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+            const uint32_t v = __shfl_up(sum, off);
+            sum += lane >= off ? v : 0;
+        }
+        if (lane == kWave - 1) wave_sum[wave] = sum;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) sum += wave_sum[w];
+        if (c < digits) base[c] += sum - t0 - t1;
+        if (c + 1 < digits) base[c + 1] += sum - t1;
+    }
+    const int64_t begin = (int64_t)blockIdx.x * a.piece, end = min(begin + a.piece, a.n);
+    for (int64_t tile = begin; tile < end; tile += kSortTile) {
+        for (int c = threadIdx.x; c < digits * kSortWaves; c += kSortBlock) count[c >> a.bits][c & (digits - 1)] = 0;
+        __syncthreads();                                   // (base is complete, and count clear)
+        uint32_t key[kSortRounds], rank[kSortRounds];
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) {
+            const int64_t i = tile + (wave * kSortRounds + r) * kWave + lane;
+            key[r] = i < end ? sort_key<I, FIRST>(a, i) : 0;
+        }
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) {
+            const bool here = tile + (wave * kSortRounds + r) * kWave + lane < end;
+            const uint32_t digit = key[r] >> a.shift & (digits - 1);
+            const uint64_t same = equal_digits(digit, a.bits, __ballot(here));
+            const int leader = same ? __builtin_ctzll(same) : lane;
+            uint32_t before = 0;
+            if (here && lane == leader) before = atomicAdd(&count[wave][digit], (uint32_t)__popcll(same));
+            rank[r] = __shfl(before, leader) + __popcll(same & ((1ull << lane) - 1));
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < digits; c += kSortBlock) {   // counts of a digit: what comes before each wavefront
+            uint32_t sum = base[c];
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t v = count[w][c];
+                count[w][c] = sum;
+                sum += v;
+            }
+            base[c] = sum;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) {
+            const int64_t i = tile + (wave * kSortRounds + r) * kWave + lane;
+            if (i >= end) continue;
+            const uint32_t to = count[wave][key[r] >> a.shift & (digits - 1)] + rank[r];
+            a.keys_out[to] = key[r];
+            a.tokens_out[to] = FIRST ? (uint32_t)i : a.tokens[i];
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------------ sums of sorted tokens
+
+struct GradArgs {
+    const void *gy;
+    int64_t stride, extent;
+    const uint32_t *keys, *tokens;   // sorted
+    void *out;
+    uint32_t *where;                 // [rows]: for every row that is named, an entry that names it; for others anything
+    float *part;                     // [workgroups][2][d]: sums of runs that began before the workgroup's entries, that go on after them
+    int64_t n, rows;
+    int32_t d, each;                 // entries of a group of lanes
+    int32_t groups;                  // workgroups of the sums
+    float scale;
+};
+
+// Adds up runs of equal keys among `count` entries in LDS (sorted; keys[-1] is the key before them, keys[count] the one after, kNone where there is none).  Groups of LPR lanes take
+// `each` entries one after the other, requesting eight rows ahead; a run inside a group's entries is done there (store), those that cross groups go through LDS
+// (edge: [groups of lanes][LPR * V] sums of the run that began earlier and ends in the group or covers it, last: the same of the run at its end) and are
+// added up by the group in which they begin.  open(first, sum): a run that began before the entries (first) or goes on after them.
+constexpr uint32_t kNone = 0xffffffffu;
+template <typename T, int LPR, bool TAIL, typename Store, typename Open>
+__device__ __forceinline__ void sum_runs(const T *gy, int64_t stride, int64_t extent, int d, int col, const uint32_t *keys, const uint32_t *tokens, int count, int each, uint32_t rows,
+                                         float (*edge)[LPR * kVec<T>], uint8_t *covered, Store store, Open open) {
+    constexpr int V = kVec<T>, G = kBlock / LPR, kAhead = 8;
+    const int l = threadIdx.x % LPR, g = threadIdx.x / LPR;
+    const int begin = min(g * each, count), end = min(begin + each, count);
+    float sum[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] = 0.f;
+    uint32_t run = begin < end ? keys[begin] : kNone;
+    bool inherited = begin < end && keys[begin - 1] == run;         // the run at hand began before this group
+    for (int i = begin; i < end; i += kAhead) {
+        typename VecOf<T>::type raw[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int at = min(i + u, end - 1);
+            raw[u] = load_columns<T, TAIL>(gy, (int64_t)tokens[at] * stride, col, d, extent);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (i + u >= end) break;
+            const uint32_t key = keys[i + u];
+            if (key != run) {
+                if (inherited) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) edge[g][l * V + e] = sum[e];
+                } else if (run != rows) {
+                    store(run, sum);
+                }
+                run = key;
+                inherited = false;
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += (float)raw[u][e];
+        }
+    }
+    const bool covers = begin < end && inherited;          // one run throughout, which began earlier
+    if (covers) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) edge[g][l * V + e] = sum[e];
+    }
+    if (l == 0) covered[g] = covers;
+    __syncthreads();
+    // the runs that are not done: one that begins in this group and reaches its end, and, for the first group, one that began before all entries
+    auto follow = [&](int from, uint32_t key, float (&s)[V]) {      // true: goes on after the last entry
+        for (int h = from; h < G; ++h) {
+            if (h * each >= count || keys[h * each] != key) return false;
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[e] += edge[h][l * V + e];
+            if (!covered[h]) return false;
+        }
+        return keys[count] == key;
+    };
+    if (g == 0 && count > 0 && keys[-1] == keys[0] && keys[0] != rows) {
+        float s[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] = 0.f;
+        follow(0, keys[0], s);
+        open(true, s);
+    }
+    if (begin < end && !inherited && run != rows) {
+        if (follow(g + 1, run, sum)) open(false, sum);
+        else store(run, sum);
+    }
+}
+
+constexpr int kEachMost = 32;
+template <typename T, typename O, int LPR, bool TAIL>
+__global__ __launch_bounds__(kBlock) void embed_sum_kernel(GradArgs a) {
+    constexpr int V = kVec<T>, G = kBlock / LPR, kMost = G * kEachMost;
+    __shared__ uint32_t key_store[kMost + 2], tokens[kMost];
+    __shared__ float edge[G][LPR * V];
+    __shared__ uint8_t covered[G];
+    uint32_t *keys = key_store + 1;
+    const int l = threadIdx.x % LPR, col = ((int)blockIdx.y * LPR + l) * V;
+    const int64_t begin = (int64_t)blockIdx.x * G * a.each;
+    const int count = (int)min((int64_t)G * a.each, a.n - begin);
+    for (int i = (int)threadIdx.x - 1; i <= count; i += kBlock) {
+        const int64_t at = begin + i;
+        keys[i] = at >= 0 && at < a.n ? a.keys[at] : kNone;
+        if (i >= 0 && i < count) tokens[i] = a.tokens[at];
+    }
+    __syncthreads();
+    if (keys[0] == (uint32_t)a.rows) return;               // nothing here names a row
+    if (blockIdx.y == 0) {
+        for (int i = threadIdx.x; i < count; i += kBlock)
+            if (keys[i] != keys[i - 1] && keys[i] != (uint32_t)a.rows) a.where[keys[i]] = (uint32_t)(begin + i);
+    }
+    sum_runs<T, LPR, TAIL>((const T *)a.gy, a.stride, a.extent, a.d, col, keys, tokens, count, a.each, (uint32_t)a.rows, edge, covered,
+        [&](uint32_t row, float (&s)[V]) {
+            if (col >= a.d) return;
+            float v[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = a.scale * s[e];
+            store_cols((O *)a.out + (int64_t)row * a.d + col, TAIL ? a.d - col : V, v);
+        },
+        [&](bool first, float (&s)[V]) {
+            if (col >= a.d) return;
+            store_cols(a.part + ((int64_t)blockIdx.x * 2 + (first ? 0 : 1)) * a.d + col, TAIL ? a.d - col : V, s);
+        });
+}
+
+// The first `groups` - 1 workgroups: the run that begins among the entries of workgroup b of the sums and goes on after them.  The others: 64 rows of g_table for each wavefront, zeros
+// where no token names them.
+template <typename T, typename O, int LPR, bool TAIL>
+__global__ __launch_bounds__(kBlock) void embed_join_kernel(GradArgs a) {
+    constexpr int V = kVec<T>, G = kBlock / LPR;
+    __shared__ float lds[G][LPR * V];
+    const int l = threadIdx.x % LPR, g = threadIdx.x / LPR;
+    if ((int)blockIdx.x < a.groups - 1) {
+        const int64_t per = (int64_t)G * a.each, begin = (int64_t)blockIdx.x * per, next = begin + per;
+        const uint32_t run = a.keys[next - 1];
+        if (run == (uint32_t)a.rows || a.keys[next] != run) return;
+        if (a.keys[begin] == run && begin > 0 && a.keys[begin - 1] == run) return;                       // it began earlier
+        // the workgroups that it reaches: those whose first entry is of this run
+        int64_t lo = blockIdx.x + 1, hi = a.groups;        // lo: reached, hi: not
+        for (int64_t step = 1; lo + step < hi; step *= 2) {
+            if (a.keys[(lo + step) * per] != run) { hi = lo + step; break; }
+            lo += step;
+        }
+        while (hi - lo > 1) {
+            const int64_t mid = (lo + hi) / 2;
+            if (a.keys[mid * per] == run) lo = mid; else hi = mid;
+        }
+        const int col = ((int)blockIdx.y * LPR + l) * V;
+        float s[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] = 0.f;
+        if (col < a.d) {
+#pragma unroll 4
+            for (int64_t b = (int64_t)blockIdx.x + g; b <= lo; b += G) {
+                const float *p = a.part + (b * 2 + (b == blockIdx.x ? 1 : 0)) * a.d + col;
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[e] += !TAIL || col + e < a.d ? p[e] : 0.f;
             }
         }
-        if (c < d) out[v * d + c] = (O)(scale * sum);
+#pragma unroll
+        for (int e = 0; e < V; ++e) lds[g][l * V + e] = s[e];
+        __syncthreads();
+        if (g > 0 || col >= a.d) return;
+        for (int h = 1; h < G && (int64_t)blockIdx.x + h <= lo; ++h)
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[e] += lds[h][l * V + e];
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] *= a.scale;
+        store_cols((O *)a.out + (int64_t)run * a.d + col, TAIL ? a.d - col : V, s);
+        return;
     }
+    if (blockIdx.y > 0) return;
+    const int lane = threadIdx.x % kWave;
+    const int64_t row0 = ((int64_t)((int)blockIdx.x - max(a.groups - 1, 0)) * (kBlock / kWave) + threadIdx.x / kWave) * kWave, row = row0 + lane;
+    bool empty = row < a.rows;
+    if (empty && a.n > 0) {
+        const uint32_t at = a.where[row];
+        empty = at >= (uint64_t)a.n || a.keys[at] != (uint32_t)row;
+    }
+    const float zero[V] = {};
+    uint64_t rest = __ballot(empty);
+    for (; rest; ) {                                       // kWave / LPR of them at a time
+        uint64_t mine = rest;
+        for (int k = 0; k < lane / LPR; ++k) mine &= mine - 1;
+        if (mine) {
+            O *p = (O *)a.out + (row0 + __builtin_ctzll(mine)) * a.d;
+            for (int col = l * V; col < a.d; col += LPR * V) store_cols(p + col, a.d - col, zero);
+        }
+        for (int k = 0; k < kWave / LPR; ++k) rest &= rest - 1;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------------ few tokens
+
+// Up to kFew tokens: one launch.  A workgroup looks through all ids for those of its 32 rows, sorts them by row in LDS and adds up their runs, which are whole.
+constexpr int kFew = 1024, kFewRows = 32, kFewRounds = kFew / kBlock;
+template <typename T, typename O, typename I, int LPR, bool TAIL>
+__global__ __launch_bounds__(kBlock) void embed_few_kernel(GradArgs a, const I *ids, int64_t padding) {
+    constexpr int V = kVec<T>, G = kBlock / LPR, kWaves = kBlock / kWave;
+    __shared__ uint32_t key_store[kFew + 2], tokens[kFew], count[kWaves][kFewRows], begins[kFewRows + 1];
+    __shared__ float edge[G][LPR * V];
+    __shared__ uint8_t covered[G];
+    uint32_t *keys = key_store + 1;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, l = threadIdx.x % LPR, g = threadIdx.x / LPR;
+    const int64_t row0 = (int64_t)blockIdx.x * kFewRows;
+    for (int c = threadIdx.x; c < kWaves * kFewRows; c += kBlock) count[c / kFewRows][c % kFewRows] = 0;
+    __syncthreads();
+    uint32_t row[kFewRounds], rank[kFewRounds];
+#pragma unroll
+    for (int r = 0; r < kFewRounds; ++r) {
+        const int i = (wave * kFewRounds + r) * kWave + lane;
+        const int64_t id = i < a.n ? (int64_t)ids[i] : -1;
+        row[r] = id >= row0 && id < a.rows && id != padding && id - row0 < kFewRows ? (uint32_t)(id - row0) : kNone;
+    }
+#pragma unroll
+    for (int r = 0; r < kFewRounds; ++r) {
+        const bool here = row[r] != kNone;
+        const uint64_t any = __ballot(here);
+        rank[r] = 0;
+        if (!any) continue;
+        const uint64_t same = equal_digits(row[r], 5, any);
+        const int leader = here ? __builtin_ctzll(same) : lane;
+        uint32_t before = 0;
+        if (here && lane == leader) before = atomicAdd(&count[wave][row[r]], (uint32_t)__popcll(same));
+        rank[r] = __shfl(before, leader) + __popcll(same & ((1ull << lane) - 1));
+    }
+    __syncthreads();
+    if (wave == 0) {
+        uint32_t sum = 0;
+        if (lane < kFewRows)
+            for (int w = 0; w < kWaves; ++w) sum += count[w][lane];
+        const uint32_t mine = sum;
+#pragma unroll
+        for (int off = 1; off < kFewRows; off <<= 1) {
+            const uint32_t v = __shfl_up(sum, off);
+            sum += lane >= off ? v : 0;
+        }
+        if (lane < kFewRows) {
+            begins[lane + 1] = sum;
+            if (lane == 0) begins[0] = 0;
+            uint32_t at = sum - mine;
+            for (int w = 0; w < kWaves; ++w) {
+                const uint32_t v = count[w][lane];
+                count[w][lane] = at;
+                at += v;
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kFewRounds; ++r)
+        if (row[r] != kNone) {
+            const uint32_t to = count[wave][row[r]] + rank[r];
+            keys[to] = row[r];
+            tokens[to] = (uint32_t)((wave * kFewRounds + r) * kWave + lane);
+        }
+    const int found = (int)begins[kFewRows];
+    if (threadIdx.x == 0) keys[-1] = keys[found] = kNone;
+    __syncthreads();
+    O *out = (O *)a.out + row0 * a.d;
+    const float zero[V] = {};
+    for (int r = g; r < kFewRows && row0 + r < a.rows; r += G)
+        if (begins[r] == begins[r + 1])
+            for (int col = l * V; col < a.d; col += LPR * V) store_cols(out + (int64_t)r * a.d + col, a.d - col, zero);
+    if (found == 0) return;
+    const int each = (found + G - 1) / G;
+    for (int col0 = 0; col0 < a.d; col0 += LPR * V) {
+        const int col = col0 + l * V;
+        sum_runs<T, LPR, TAIL>((const T *)a.gy, a.stride, a.extent, a.d, col, keys, tokens, found, each, kNone, edge, covered,
+            [&](uint32_t r, float (&s)[V]) {
+                if (col >= a.d) return;
+                float v[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = a.scale * s[e];
+                store_cols(out + (int64_t)r * a.d + col, TAIL ? a.d - col : V, v);
+            },
+            [&](bool, float (&)[V]) {});
+        __syncthreads();                                   // (edge is used again)
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------------ sizes
+
+static int embed_lanes(int64_t d, int vec) {
+    int lpr = 4;
+    while (lpr < kWave && lpr * vec < d) lpr *= 2;
+    return lpr;
+}
+template <typename F>
+static int lanes_switch(int lpr, bool tail, F f) {
+    auto with = [&](auto n) { return tail ? f(n, std::true_type()) : f(n, std::false_type()); };
+    return lpr == 4    ? with(std::integral_constant<int, 4>())
+           : lpr == 8  ? with(std::integral_constant<int, 8>())
+           : lpr == 16 ? with(std::integral_constant<int, 16>())
+           : lpr == 32 ? with(std::integral_constant<int, 32>())
+                       : with(std::integral_constant<int, 64>());
+}
+
+// The parts of a gradient's workspace.
+struct GradPlan {
+    int64_t piece;               // sort
+    int32_t pieces, passes, bits;
+    int32_t each, groups;        // sums
+    size_t lists, counts, where, part, bytes;      // offsets; four lists of n words begin at `lists`
+};
+static GradPlan grad_plan(int64_t n, int64_t rows, int64_t d, int vec) {
+    GradPlan p = {};
+    int key_bits = 1;
+    while ((rows >> key_bits) > 0) ++key_bits;
+    p.passes = (key_bits + kSortBits - 1) / kSortBits;
+    p.bits = (key_bits + p.passes - 1) / p.passes;
+    p.piece = std::max<int64_t>(1, (n + (int64_t)kSortPieces * kSortTile - 1) / ((int64_t)kSortPieces * kSortTile)) * kSortTile;
+    p.pieces = (int32_t)((n + p.piece - 1) / p.piece);
+    const int64_t side = kBlock / embed_lanes(d, vec);
+    p.each = kEachMost;
+    while (p.each > 8 && n < side * p.each * 1024) p.each /= 2;
+    p.groups = (int32_t)((n + side * p.each - 1) / (side * p.each));
+    auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += (bytes + 255) / 256 * 256; return at; };
+    p.lists = take((size_t)n * 4 * 4);
+    p.counts = take((size_t)p.pieces * 4 << p.bits);
+    p.where = take((size_t)rows * 4);
+    p.part = take((size_t)p.groups * 2 * d * 4);
+    return p;
 }
 
 }  // namespace hag
@@ -58,22 +526,25 @@ int hag_embedding(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, const v
     if (!elem_type(dtype)) { set_error("elements are HAG_F32, HAG_BF16 or HAG_F16"); return HAG_EINVAL; }
     if (n == 0) return HAG_OK;
     if ((rows > 0 && !table) || !ids || !y) { set_error("NULL pointer"); return HAG_EINVAL; }
-    const unsigned groups = (unsigned)((n + 3) / 4);
+    const EmbedArgs a = {table, ids, y, table_stride, rows > 0 ? (rows - 1) * table_stride + d : 0, n, rows, padding, (int32_t)d, scale};
     return elem_switch(dtype, [&](auto e) {
         return id_switch(id_type, [&](auto k) {
             using T = decltype(e);
             using I = decltype(k);
-            hipLaunchKernelGGL((embed_kernel<T, I>), dim3(groups), dim3(kBlock), 0, (hipStream_t)stream, (const T *)table, table_stride, (const I *)ids, n, rows, (int32_t)d,
-                               padding, scale, (T *)y);
-            HIP_TRY(hipGetLastError());
-            return (int)HAG_OK;
+            return lanes_switch(embed_lanes(d, kVec<T>), d % kVec<T> != 0, [&](auto lanes, auto tail) {
+                constexpr int LPR = decltype(lanes)::value;
+                constexpr int64_t kRows = kBlock / LPR * kEmbedRows;
+                hipLaunchKernelGGL((embed_kernel<T, I, LPR, decltype(tail)::value>), dim3((unsigned)((n + kRows - 1) / kRows)), dim3(kBlock), 0, (hipStream_t)stream, a);
+                HIP_TRY(hipGetLastError());
+                return (int)HAG_OK;
+            });
         });
     });
 }
 
 size_t hag_embedding_grad_workspace_bytes(int64_t n, int64_t rows, int64_t d) {
     if (embed_refusal(n, rows, d, HAG_I64, 0)) return 0;
-    return 16;
+    return n <= kFew ? 16 : std::max(grad_plan(n, rows, d, 4).bytes, grad_plan(n, rows, d, 8).bytes);
 }
 
 int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, const void *g_y, int64_t g_y_stride, hag_dtype_t id_type, const void *ids, int64_t padding,
@@ -86,19 +557,78 @@ int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, co
     if (rows == 0) return HAG_OK;
     if ((n > 0 && (!g_y || !ids)) || !g_table || !workspace) { set_error("NULL pointer"); return HAG_EINVAL; }
     if ((uintptr_t)workspace & 15) { set_error("workspace must be 16-byte aligned"); return HAG_EINVAL; }
-    return elem_switch(dtype, [&](auto e) {
-        return id_switch(id_type, [&](auto k) {
-            using T = decltype(e);
-            using I = decltype(k);
-            auto launch = [&](auto o) {
-                using O = decltype(o);
-                hipLaunchKernelGGL((embed_grad_kernel<T, O, I>), dim3((unsigned)((rows + 3) / 4)), dim3(kBlock), 0, (hipStream_t)stream, (const T *)g_y, g_y_stride, (const I *)ids,
-                                   n, rows, (int32_t)d, padding, scale, (O *)g_table);
+    hipStream_t s = (hipStream_t)stream;
+    GradArgs a = {};
+    a.gy = g_y;
+    a.stride = g_y_stride;
+    a.extent = n > 0 ? (n - 1) * g_y_stride + d : 0;
+    a.out = g_table;
+    a.n = n;
+    a.rows = rows;
+    a.d = (int32_t)d;
+    a.scale = scale;
+    const int vec = 16 / elem_size(dtype), lpr = embed_lanes(d, vec);
+    const bool tail = d % vec != 0;
+    const unsigned chunks = (unsigned)((d + lpr * vec - 1) / (lpr * vec));
+    // f(type of g_y, of g_table, lanes, tail)
+    auto pick = [&](auto f) {
+        return elem_switch(dtype, [&](auto e) {
+            return lanes_switch(lpr, tail, [&](auto lanes, auto tails) { return out_dtype == dtype ? f(e, e, lanes, tails) : f(e, float(), lanes, tails); });
+        });
+    };
+    if (n <= kFew)
+        return pick([&](auto e, auto o, auto lanes, auto tails) {
+            return id_switch(id_type, [&](auto k) {
+                using I = decltype(k);
+                hipLaunchKernelGGL((embed_few_kernel<decltype(e), decltype(o), I, decltype(lanes)::value, decltype(tails)::value>), dim3((unsigned)((rows + kFewRows - 1) / kFewRows)),
+                                   dim3(kBlock), 0, s, a, (const I *)ids, padding);
                 HIP_TRY(hipGetLastError());
                 return (int)HAG_OK;
-            };
-            return out_dtype == dtype ? launch(T()) : launch(float());
+            });
         });
+    const GradPlan p = grad_plan(n, rows, d, vec);
+    char *ws = (char *)workspace;
+    uint32_t *lists = (uint32_t *)(ws + p.lists);
+    SortArgs sort = {};
+    sort.ids = ids;
+    sort.counts = (uint32_t *)(ws + p.counts);
+    sort.n = n;
+    sort.rows = rows;
+    sort.padding = padding;
+    sort.piece = p.piece;
+    sort.pieces = p.pieces;
+    sort.bits = p.bits;
+    for (int pass = 0; pass < p.passes; ++pass) {
+        sort.shift = pass * p.bits;
+        sort.keys = sort.keys_out;
+        sort.tokens = sort.tokens_out;
+        sort.keys_out = lists + (pass & 1) * 2 * n;
+        sort.tokens_out = sort.keys_out + n;
+        typedef void (*kernel_t)(SortArgs);
+        const kernel_t count = pass > 0 ? (kernel_t)sort_count_kernel<int32_t, false> : id_type == HAG_I64 ? (kernel_t)sort_count_kernel<int64_t, true> : (kernel_t)sort_count_kernel<int32_t, true>;
+        const kernel_t place = pass > 0 ? (kernel_t)sort_place_kernel<int32_t, false> : id_type == HAG_I64 ? (kernel_t)sort_place_kernel<int64_t, true> : (kernel_t)sort_place_kernel<int32_t, true>;
+        hipLaunchKernelGGL(count, dim3((unsigned)p.pieces), dim3(kSortBlock), 0, s, sort);
+        HIP_TRY(hipGetLastError());
+        hipLaunchKernelGGL(place, dim3((unsigned)p.pieces), dim3(kSortBlock), 0, s, sort);
+        HIP_TRY(hipGetLastError());
+    }
+    a.keys = sort.keys_out;
+    a.tokens = sort.tokens_out;
+    a.where = (uint32_t *)(ws + p.where);
+    a.part = (float *)(ws + p.part);
+    a.each = p.each;
+    a.groups = p.groups;
+    const unsigned joins = (unsigned)(p.groups - 1) + (unsigned)((rows + kBlock - 1) / kBlock);
+    return pick([&](auto e, auto o, auto lanes, auto tails) {
+        using T = decltype(e);
+        using O = decltype(o);
+        constexpr int LPR = decltype(lanes)::value;
+        constexpr bool TAIL = decltype(tails)::value;
+        hipLaunchKernelGGL((embed_sum_kernel<T, O, LPR, TAIL>), dim3((unsigned)p.groups, chunks), dim3(kBlock), 0, s, a);
+        HIP_TRY(hipGetLastError());
+        hipLaunchKernelGGL((embed_join_kernel<T, O, LPR, TAIL>), dim3(joins, chunks), dim3(kBlock), 0, s, a);
+        HIP_TRY(hipGetLastError());
+        return (int)HAG_OK;
     });
 }
 

@@ -42,14 +42,6 @@ __device__ __forceinline__ void load_params(const void *p, int param32, int col,
     }
 }
 
-// Columns col .. col + kVec of the row at element `at`; lanes beyond the row's end get its first ones, so that no load waits for a condition.  TAIL: d is no multiple
-// of the vector, a row's last vector brings elements of the next row along, and at the end of the matrix is read element by element.
-template <typename T, bool TAIL>
-__device__ __forceinline__ typename VecOf<T>::type load_columns(const T *base, int64_t at, int col, int d, int64_t extent) {
-    const T *p = base + at + (col < d ? col : 0);
-    return TAIL ? load_vec(p, p - base + kVec<T> <= extent, d - col) : load_vec(p);
-}
-
 // Sums over a row, in all of its lanes.  Rows of up to 64 lanes: moves between lanes; longer ones: the workgroup, through LDS (two halves, used in turn, so that one barrier
 // a sum is enough).
 template <int LPR>
