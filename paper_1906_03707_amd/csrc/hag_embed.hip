@@ -58,7 +58,9 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
 
 // A token's key is its id, `rows` where it names no row: those come last and are left out.  Radix sort, low digits first, with stable passes of up to 10 bits:
 // counts per piece of the list, then every piece finds where each of its digits begins (the counts of smaller digits and of earlier pieces) and writes its tokens there.
-constexpr int kSortBlock = 512, kSortWaves = kSortBlock / kWave, kSortRounds = 8, kSortTile = kSortBlock * kSortRounds, kSortBits = 10, kSortPieces = 128;
+// Few bytes, so what it costs is the way of a piece through the steps of a pass: many loads at a time, few pieces to look back at.
+constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / kWave, kSortRounds = 4, kSortTile = kSortBlock * kSortRounds, kSortBits = 10, kSortPieces = 128;
+constexpr int kSortAlone = 4;        // so few pieces count the others' tokens themselves
 struct SortArgs {
     const void *ids;                 // first pass: the tokens' ids
     const uint32_t *keys, *tokens;   // later passes: what the one before wrote
@@ -67,14 +69,11 @@ struct SortArgs {
     int32_t pieces, shift, bits;
 };
 
-template <typename I>
-__device__ __forceinline__ uint32_t token_key(const I *ids, int64_t i, int64_t rows, int64_t padding) {
-    const int64_t id = ids[i];
-    return id >= 0 && id < rows && id != padding ? (uint32_t)id : (uint32_t)rows;
-}
 template <typename I, bool FIRST>
 __device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int64_t i) {
-    return FIRST ? token_key((const I *)a.ids, i, a.rows, a.padding) : a.keys[i];
+    if (!FIRST) return a.keys[i];
+    const int64_t id = ((const I *)a.ids)[i];
+    return id >= 0 && id < a.rows && id != a.padding ? (uint32_t)id : (uint32_t)a.rows;
 }
 
 // lanes whose digit is this lane's, among those of `active`
@@ -87,97 +86,151 @@ __device__ __forceinline__ uint64_t equal_digits(uint32_t digit, int bits, uint6
     return active;
 }
 
+// sum over the threads before this one; all threads of the workgroup take part
+__device__ __forceinline__ uint32_t threads_before(uint32_t v, uint32_t *wave_sum) {
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    uint32_t sum = v;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+        const uint32_t u = __shfl_up(sum, off);
+        sum += lane >= off ? u : 0;
+    }
+    if (lane == kWave - 1) wave_sum[wave] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) before += w < wave ? wave_sum[w] : 0;
+    return before + sum - v;
+}
+
+// count[digit] of the tokens begin .. end
+template <typename I, bool FIRST>
+__device__ __forceinline__ void count_digits(const SortArgs &a, int64_t begin, int64_t end, uint32_t *count) {
+    for (int64_t tile = begin; tile < end; tile += kSortTile) {
+        uint32_t key[kSortRounds];
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) key[r] = sort_key<I, FIRST>(a, min(tile + r * kSortBlock + threadIdx.x, end - 1));
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r)
+            if (tile + r * kSortBlock + threadIdx.x < end) atomicAdd(&count[key[r] >> a.shift & ((1u << a.bits) - 1)], 1u);
+    }
+}
+
 template <typename I, bool FIRST>
 __global__ __launch_bounds__(kSortBlock) void sort_count_kernel(SortArgs a) {
     __shared__ uint32_t count[1 << kSortBits];
     const int digits = 1 << a.bits;
-    for (int c = threadIdx.x; c < digits; c += kSortBlock) count[c] = 0;
+    if ((int)threadIdx.x < digits) count[threadIdx.x] = 0;
     __syncthreads();
-    const int64_t begin = (int64_t)blockIdx.x * a.piece, end = min(begin + a.piece, a.n);
-    for (int64_t i = begin + threadIdx.x; i < end; i += kSortBlock) atomicAdd(&count[sort_key<I, FIRST>(a, i) >> a.shift & (digits - 1)], 1u);
+    const int64_t begin = (int64_t)blockIdx.x * a.piece;
+    count_digits<I, FIRST>(a, begin, min(begin + a.piece, a.n), count);
     __syncthreads();
-    for (int c = threadIdx.x; c < digits; c += kSortBlock) a.counts[(int64_t)blockIdx.x * digits + c] = count[c];
+    if ((int)threadIdx.x < digits) a.counts[(int64_t)blockIdx.x * digits + threadIdx.x] = count[threadIdx.x];
 }
 
-// Within a tile a wavefront takes 512 tokens in their order, 64 at a time; a token's place is where its digit begins, plus the tokens of that digit in earlier
-// wavefronts of the tile, in earlier rounds of its own, and in lower lanes.
+// Within a tile a wavefront takes 256 tokens in their order, 64 at a time; a token's place in the tile is where its digit begins, plus the tokens of that digit in earlier wavefronts, in
+// earlier rounds of its own, and in lower lanes.  The tile is put in that order in LDS first, so that neighbours are written side by side.
 template <typename I, bool FIRST>
 __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
-    __shared__ uint32_t count[kSortWaves][1 << kSortBits], base[1 << kSortBits], total[1 << kSortBits], wave_sum[kSortWaves];
-    const int digits = 1 << a.bits, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    for (int c = threadIdx.x; c < digits; c += kSortBlock) base[c] = total[c] = 0;
-    __syncthreads();
-    {
-        const int slices = max(1, kSortBlock >> a.bits);
-        for (int c = threadIdx.x; c < digits * slices; c += kSortBlock) {
-            const int digit = c & (digits - 1);
-            uint32_t all = 0, before = 0;
-#pragma unroll 16
-            for (int p = c >> a.bits; p < a.pieces; p += slices) {
-                const uint32_t v = a.counts[(int64_t)p * digits + digit];
-                all += v;
-                before += p < (int)blockIdx.x ? v : 0;
-            }
-            atomicAdd(&total[digit], all);
-            atomicAdd(&base[digit], before);
-        }
-    }
-    __syncthreads();
-    {   // base[digit] += tokens of smaller digits: two digits a thread, then lanes, then wavefronts
-        const int c = 2 * threadIdx.x;
-        const uint32_t t0 = c < digits ? total[c] : 0, t1 = c + 1 < digits ? total[c + 1] : 0;
-        uint32_t sum = t0 + t1;
-#pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const uint32_t v = __shfl_up(sum, off);
-            sum += lane >= off ? v : 0;
-        }
-        if (lane == kWave - 1) wave_sum[wave] = sum;
-        __syncthreads();
-        for (int w = 0; w < wave; ++w) sum += wave_sum[w];
-        if (c < digits) base[c] += sum - t0 - t1;
-        if (c + 1 < digits) base[c + 1] += sum - t1;
-    }
+    __shared__ uint32_t space[2 * kSortTile];              // counts per wavefront and digit, 16 bits each; then the tile's keys and tokens in order
+    __shared__ uint32_t base[1 << kSortBits], total[1 << kSortBits], wave_sum[2][kSortWaves];
+    static_assert(kSortWaves << kSortBits <= 4 * kSortTile, "counts of 16 bits in the space of the tile");
+    uint16_t *count = (uint16_t *)space;
+    const int digits = 1 << a.bits, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, mine = threadIdx.x;
     const int64_t begin = (int64_t)blockIdx.x * a.piece, end = min(begin + a.piece, a.n);
-    for (int64_t tile = begin; tile < end; tile += kSortTile) {
-        for (int c = threadIdx.x; c < digits * kSortWaves; c += kSortBlock) count[c >> a.bits][c & (digits - 1)] = 0;
-        __syncthreads();                                   // (base is complete, and count clear)
-        uint32_t key[kSortRounds], rank[kSortRounds];
+    uint32_t key[kSortRounds], token[kSortRounds];
+    auto request = [&](int64_t tile) {
 #pragma unroll
         for (int r = 0; r < kSortRounds; ++r) {
-            const int64_t i = tile + (wave * kSortRounds + r) * kWave + lane;
-            key[r] = i < end ? sort_key<I, FIRST>(a, i) : 0;
+            const int64_t i = min(tile + (wave * kSortRounds + r) * kWave + lane, end - 1);
+            key[r] = sort_key<I, FIRST>(a, i);
+            token[r] = FIRST ? (uint32_t)i : a.tokens[i];
         }
+    };
+    request(begin);
+    if (mine < digits) base[mine] = total[mine] = 0;
+    __syncthreads();
+    // total: tokens of every digit; base: those of earlier pieces
+    if (a.pieces <= kSortAlone) {
+        count_digits<I, FIRST>(a, 0, begin, base);
+        count_digits<I, FIRST>(a, begin, a.n, total);
+        __syncthreads();
+        if (mine < digits) total[mine] += base[mine];
+    } else {
+        const int slices = kSortBlock >> a.bits, digit = mine & (digits - 1);
+        uint32_t all = 0, before = 0;
+        for (int p0 = mine >> a.bits; p0 < a.pieces; p0 += 16 * slices) {
+            uint32_t v[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) v[u] = a.counts[(int64_t)min(p0 + u * slices, a.pieces - 1) * digits + digit];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+                const int p = p0 + u * slices;
+                all += p < a.pieces ? v[u] : 0;
+                before += p < (int)blockIdx.x ? v[u] : 0;
+            }
+        }
+        atomicAdd(&total[digit], all);
+        atomicAdd(&base[digit], before);
+        __syncthreads();
+    }
+    {
+        const uint32_t smaller = threads_before(mine < digits ? total[mine] : 0, wave_sum[0]);
+        if (mine < digits) base[mine] += smaller;
+    }
+    for (int64_t tile = begin; tile < end; tile += kSortTile) {
+        if (tile > begin) request(tile);
+        for (int c = mine; c < (kSortWaves << a.bits) / 2; c += kSortBlock) space[c] = 0;
+        __syncthreads();
+        uint32_t place[kSortRounds];
 #pragma unroll
         for (int r = 0; r < kSortRounds; ++r) {
             const bool here = tile + (wave * kSortRounds + r) * kWave + lane < end;
-            const uint32_t digit = key[r] >> a.shift & (digits - 1);
+            const uint32_t digit = key[r] >> a.shift & (digits - 1), at = (uint32_t)wave << a.bits | digit;
             const uint64_t same = equal_digits(digit, a.bits, __ballot(here));
             const int leader = same ? __builtin_ctzll(same) : lane;
             uint32_t before = 0;
-            if (here && lane == leader) before = atomicAdd(&count[wave][digit], (uint32_t)__popcll(same));
-            rank[r] = __shfl(before, leader) + __popcll(same & ((1ull << lane) - 1));
+            if (here && lane == leader) before = atomicAdd(&space[at >> 1], (uint32_t)__popcll(same) << (at & 1) * 16) >> (at & 1) * 16 & 0xffff;
+            place[r] = __shfl(before, leader) + __popcll(same & ((1ull << lane) - 1));
         }
         __syncthreads();
-        for (int c = threadIdx.x; c < digits; c += kSortBlock) {   // counts of a digit: what comes before each wavefront
-            uint32_t sum = base[c];
+        uint32_t here = 0;                                 // the tile's tokens of digit `mine`
+        if (mine < digits) {
+            uint32_t v[kSortWaves];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) v[w] = count[w << a.bits | mine];
+#pragma unroll
             for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t v = count[w][c];
-                count[w][c] = sum;
-                sum += v;
+                count[w << a.bits | mine] = (uint16_t)here;
+                here += v[w];
             }
-            base[c] = sum;
+        }
+        const uint32_t smaller = threads_before(here, wave_sum[1]);
+        if (mine < digits) {
+            total[mine] = smaller;                         // (where the digit begins in the tile)
         }
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kSortRounds; ++r) {
-            const int64_t i = tile + (wave * kSortRounds + r) * kWave + lane;
-            if (i >= end) continue;
-            const uint32_t to = count[wave][key[r] >> a.shift & (digits - 1)] + rank[r];
-            a.keys_out[to] = key[r];
-            a.tokens_out[to] = FIRST ? (uint32_t)i : a.tokens[i];
+            const uint32_t digit = key[r] >> a.shift & (digits - 1);
+            place[r] += total[digit] + count[wave << a.bits | digit];
         }
         __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r)
+            if (tile + (wave * kSortRounds + r) * kWave + lane < end) {
+                space[place[r]] = key[r];
+                space[kSortTile + place[r]] = token[r];
+            }
+        __syncthreads();
+        const int filled = (int)min((int64_t)kSortTile, end - tile);
+        for (int j = mine; j < filled; j += kSortBlock) {
+            const uint32_t k = space[j], digit = k >> a.shift & (digits - 1), to = base[digit] + (uint32_t)j - total[digit];
+            a.keys_out[to] = k;
+            a.tokens_out[to] = space[kSortTile + j];
+        }
+        __syncthreads();
+        if (mine < digits) base[mine] += here;
     }
 }
 
@@ -198,12 +251,11 @@ struct GradArgs {
 
 // Adds up runs of equal keys among `count` entries in LDS (sorted; keys[-1] is the key before them, keys[count] the one after, kNone where there is none).  Groups of LPR lanes take
 // `each` entries one after the other, requesting eight rows ahead; a run inside a group's entries is done there (store), those that cross groups go through LDS
-// (edge: [groups of lanes][LPR * V] sums of the run that began earlier and ends in the group or covers it, last: the same of the run at its end) and are
-// added up by the group in which they begin.  open(first, sum): a run that began before the entries (first) or goes on after them.
+// (edge: [groups of lanes][LPR * V] sums of the run that began earlier and ends in the group or covers it) and are added up by the group in which they begin.  open(first, sum): a run that began before the entries (first) or goes on after them.
 constexpr uint32_t kNone = 0xffffffffu;
 template <typename T, int LPR, bool TAIL, typename Store, typename Open>
 __device__ __forceinline__ void sum_runs(const T *gy, int64_t stride, int64_t extent, int d, int col, const uint32_t *keys, const uint32_t *tokens, int count, int each, uint32_t rows,
-                                         float (*edge)[LPR * kVec<T>], uint8_t *covered, Store store, Open open) {
+                                         float (*edge)[LPR * kVec<T>], uint8_t *flags, Store store, Open open) {
     constexpr int V = kVec<T>, G = kBlock / LPR, kAhead = 8;
     const int l = threadIdx.x % LPR, g = threadIdx.x / LPR;
     const int begin = min(g * each, count), end = min(begin + each, count);
@@ -244,27 +296,33 @@ __device__ __forceinline__ void sum_runs(const T *gy, int64_t stride, int64_t ex
 #pragma unroll
         for (int e = 0; e < V; ++e) edge[g][l * V + e] = sum[e];
     }
-    if (l == 0) covered[g] = covers;
+    // bit 0: the group's first entry goes on with the run before it; bit 1: one such run covers the group
+    if (l == 0) flags[g] = (uint8_t)((begin < end && keys[begin - 1] == keys[begin] ? 1 : 0) | (covers ? 2 : 0));
     __syncthreads();
+    const int lane = threadIdx.x % kWave;
+    const uint8_t flag = lane < G ? flags[lane] : 0;
+    const uint64_t goes_on = __ballot(flag & 1), through = __ballot(flag & 2);
     // the runs that are not done: one that begins in this group and reaches its end, and, for the first group, one that began before all entries
-    auto follow = [&](int from, uint32_t key, float (&s)[V]) {      // true: goes on after the last entry
-        for (int h = from; h < G; ++h) {
-            if (h * each >= count || keys[h * each] != key) return false;
+    auto follow = [&](int from, float (&s)[V]) {           // adds groups from, from + 1, ... as far as the run reaches; true: it goes on after the last entry
+        // the first group that begins another run, and the first where the run ends inside
+        const uint64_t other = from < 64 ? ~goes_on >> from : 1, inside = from < 64 ? ~through >> from : 1;
+        const int until = min(from + (other ? __builtin_ctzll(other) : 64), G), last = from + (inside ? __builtin_ctzll(inside) : 64);
+        const int stop = min(until, last + 1);
+#pragma unroll 4
+        for (int h = from; h < stop; ++h)
 #pragma unroll
             for (int e = 0; e < V; ++e) s[e] += edge[h][l * V + e];
-            if (!covered[h]) return false;
-        }
-        return keys[count] == key;
+        return stop == until && until * each >= count && last >= until;
     };
     if (g == 0 && count > 0 && keys[-1] == keys[0] && keys[0] != rows) {
         float s[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) s[e] = 0.f;
-        follow(0, keys[0], s);
+        follow(0, s);
         open(true, s);
     }
     if (begin < end && !inherited && run != rows) {
-        if (follow(g + 1, run, sum)) open(false, sum);
+        if (follow(g + 1, sum) && keys[count] == run) open(false, sum);
         else store(run, sum);
     }
 }
@@ -275,23 +333,30 @@ __global__ __launch_bounds__(kBlock) void embed_sum_kernel(GradArgs a) {
     constexpr int V = kVec<T>, G = kBlock / LPR, kMost = G * kEachMost;
     __shared__ uint32_t key_store[kMost + 2], tokens[kMost];
     __shared__ float edge[G][LPR * V];
-    __shared__ uint8_t covered[G];
+    __shared__ uint8_t flags[G];
     uint32_t *keys = key_store + 1;
     const int l = threadIdx.x % LPR, col = ((int)blockIdx.y * LPR + l) * V;
     const int64_t begin = (int64_t)blockIdx.x * G * a.each;
     const int count = (int)min((int64_t)G * a.each, a.n - begin);
-    for (int i = (int)threadIdx.x - 1; i <= count; i += kBlock) {
-        const int64_t at = begin + i;
-        keys[i] = at >= 0 && at < a.n ? a.keys[at] : kNone;
-        if (i >= 0 && i < count) tokens[i] = a.tokens[at];
+    for (int i = threadIdx.x; i < count; i += 2 * kBlock) {
+        const int64_t at = begin + i, then = begin + min(i + kBlock, count - 1);
+        const uint32_t k0 = a.keys[at], k1 = a.keys[then], t0 = a.tokens[at], t1 = a.tokens[then];
+        keys[i] = k0;
+        tokens[i] = t0;
+        if (i + kBlock < count) {
+            keys[i + kBlock] = k1;
+            tokens[i + kBlock] = t1;
+        }
     }
+    if (threadIdx.x == 0) keys[-1] = begin > 0 ? a.keys[begin - 1] : kNone;
+    if (threadIdx.x == kBlock - 1) keys[count] = begin + count < a.n ? a.keys[begin + count] : kNone;
     __syncthreads();
     if (keys[0] == (uint32_t)a.rows) return;               // nothing here names a row
     if (blockIdx.y == 0) {
         for (int i = threadIdx.x; i < count; i += kBlock)
             if (keys[i] != keys[i - 1] && keys[i] != (uint32_t)a.rows) a.where[keys[i]] = (uint32_t)(begin + i);
     }
-    sum_runs<T, LPR, TAIL>((const T *)a.gy, a.stride, a.extent, a.d, col, keys, tokens, count, a.each, (uint32_t)a.rows, edge, covered,
+    sum_runs<T, LPR, TAIL>((const T *)a.gy, a.stride, a.extent, a.d, col, keys, tokens, count, a.each, (uint32_t)a.rows, edge, flags,
         [&](uint32_t row, float (&s)[V]) {
             if (col >= a.d) return;
             float v[V];
@@ -314,29 +379,35 @@ __global__ __launch_bounds__(kBlock) void embed_join_kernel(GradArgs a) {
     const int l = threadIdx.x % LPR, g = threadIdx.x / LPR;
     if ((int)blockIdx.x < a.groups - 1) {
         const int64_t per = (int64_t)G * a.each, begin = (int64_t)blockIdx.x * per, next = begin + per;
-        const uint32_t run = a.keys[next - 1];
-        if (run == (uint32_t)a.rows || a.keys[next] != run) return;
-        if (a.keys[begin] == run && begin > 0 && a.keys[begin - 1] == run) return;                       // it began earlier
-        // the workgroups that it reaches: those whose first entry is of this run
-        int64_t lo = blockIdx.x + 1, hi = a.groups;        // lo: reached, hi: not
-        for (int64_t step = 1; lo + step < hi; step *= 2) {
-            if (a.keys[(lo + step) * per] != run) { hi = lo + step; break; }
-            lo += step;
-        }
-        while (hi - lo > 1) {
-            const int64_t mid = (lo + hi) / 2;
-            if (a.keys[mid * per] == run) lo = mid; else hi = mid;
+        const uint32_t run = a.keys[next - 1], first = a.keys[begin], before = begin > 0 ? a.keys[begin - 1] : kNone, after = a.keys[next];
+        // the last workgroup that it reaches: those whose first entry is of this run, 256 looked at a time (the first of them with the loads above)
+        int64_t lo = blockIdx.x;
+        uint32_t probe = a.keys[min(lo + 1 + threadIdx.x, (int64_t)a.groups - 1) * per];
+        if (run == (uint32_t)a.rows || after != run || (first == run && before == run)) return;          // padding; done; began earlier
+        for (;;) {
+            const int found = __syncthreads_count(lo + 1 + threadIdx.x < a.groups && probe == run);
+            lo += found;
+            if (found < kBlock) break;
+            probe = a.keys[min(lo + 1 + threadIdx.x, (int64_t)a.groups - 1) * per];
         }
         const int col = ((int)blockIdx.y * LPR + l) * V;
         float s[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) s[e] = 0.f;
         if (col < a.d) {
-#pragma unroll 4
-            for (int64_t b = (int64_t)blockIdx.x + g; b <= lo; b += G) {
-                const float *p = a.part + (b * 2 + (b == blockIdx.x ? 1 : 0)) * a.d + col;
+            for (int64_t b0 = (int64_t)blockIdx.x + g; b0 <= lo; b0 += 4 * G) {
+                float p[4][V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) s[e] += !TAIL || col + e < a.d ? p[e] : 0.f;
+                for (int u = 0; u < 4; ++u) {
+                    const int64_t b = min(b0 + u * G, lo);
+                    const float *q = a.part + (b * 2 + (b == blockIdx.x ? 1 : 0)) * a.d;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) p[u][e] = q[TAIL ? min(col + e, a.d - 1) : col + e];
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) s[e] += b0 + u * G <= lo ? p[u][e] : 0.f;
             }
         }
 #pragma unroll
@@ -381,7 +452,7 @@ __global__ __launch_bounds__(kBlock) void embed_few_kernel(GradArgs a, const I *
     constexpr int V = kVec<T>, G = kBlock / LPR, kWaves = kBlock / kWave;
     __shared__ uint32_t key_store[kFew + 2], tokens[kFew], count[kWaves][kFewRows], begins[kFewRows + 1];
     __shared__ float edge[G][LPR * V];
-    __shared__ uint8_t covered[G];
+    __shared__ uint8_t flags[G];
     uint32_t *keys = key_store + 1;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, l = threadIdx.x % LPR, g = threadIdx.x / LPR;
     const int64_t row0 = (int64_t)blockIdx.x * kFewRows;
@@ -448,7 +519,7 @@ __global__ __launch_bounds__(kBlock) void embed_few_kernel(GradArgs a, const I *
     const int each = (found + G - 1) / G;
     for (int col0 = 0; col0 < a.d; col0 += LPR * V) {
         const int col = col0 + l * V;
-        sum_runs<T, LPR, TAIL>((const T *)a.gy, a.stride, a.extent, a.d, col, keys, tokens, found, each, kNone, edge, covered,
+        sum_runs<T, LPR, TAIL>((const T *)a.gy, a.stride, a.extent, a.d, col, keys, tokens, found, each, kNone, edge, flags,
             [&](uint32_t r, float (&s)[V]) {
                 if (col >= a.d) return;
                 float v[V];
@@ -495,7 +566,7 @@ static GradPlan grad_plan(int64_t n, int64_t rows, int64_t d, int vec) {
     p.pieces = (int32_t)((n + p.piece - 1) / p.piece);
     const int64_t side = kBlock / embed_lanes(d, vec);
     p.each = kEachMost;
-    while (p.each > 8 && n < side * p.each * 1024) p.each /= 2;
+    while (p.each > 8 && n < side * p.each * 512) p.each /= 2;
     p.groups = (int32_t)((n + side * p.each - 1) / (side * p.each));
     auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += (bytes + 255) / 256 * 256; return at; };
     p.lists = take((size_t)n * 4 * 4);
@@ -607,7 +678,7 @@ int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, co
         typedef void (*kernel_t)(SortArgs);
         const kernel_t count = pass > 0 ? (kernel_t)sort_count_kernel<int32_t, false> : id_type == HAG_I64 ? (kernel_t)sort_count_kernel<int64_t, true> : (kernel_t)sort_count_kernel<int32_t, true>;
         const kernel_t place = pass > 0 ? (kernel_t)sort_place_kernel<int32_t, false> : id_type == HAG_I64 ? (kernel_t)sort_place_kernel<int64_t, true> : (kernel_t)sort_place_kernel<int32_t, true>;
-        hipLaunchKernelGGL(count, dim3((unsigned)p.pieces), dim3(kSortBlock), 0, s, sort);
+        if (p.pieces > kSortAlone) hipLaunchKernelGGL(count, dim3((unsigned)p.pieces), dim3(kSortBlock), 0, s, sort);
         HIP_TRY(hipGetLastError());
         hipLaunchKernelGGL(place, dim3((unsigned)p.pieces), dim3(kSortBlock), 0, s, sort);
         HIP_TRY(hipGetLastError());
