@@ -7,7 +7,8 @@
 namespace hag {
 
 // The tensors are cut into units of at most `unit` elements, one workgroup each; a launch takes as many tensors as its argument block holds.
-constexpr int kClipTensors = 112, kClipUnits = 2048;
+constexpr int kClipTensors = 112;
+constexpr int64_t kClipUnits = 2048, kClipRound = 4096;
 struct ClipArgs {
     struct Tensor {
         const void *in;
@@ -45,14 +46,34 @@ __device__ __forceinline__ double block_sum64(double v, double *lds) {
     return v;
 }
 
+// Pieces of a unit that a workgroup moves at a time: four vectors of 16 bytes for each thread, requested together.
+constexpr int kClipAsk = 4;
+template <typename T>
+constexpr int kClipPiece = kClipAsk * kBlock * kVec<T>;
+
 template <typename T>
 __device__ __forceinline__ double sum_squares(const T *p, int64_t count) {
-    double s = 0.;
-    for (int64_t i = threadIdx.x; i < count; i += kBlock) { const double v = (double)(float)p[i]; s += v * v; }
-    return s;
+    constexpr int V = kVec<T>;
+    double s[kClipAsk] = {};
+    int64_t at = 0;
+    for (; at + kClipPiece<T> <= count; at += kClipPiece<T>) {
+        typename VecOf<T>::type raw[kClipAsk];
+#pragma unroll
+        for (int u = 0; u < kClipAsk; ++u) raw[u] = load_vec(p + at + (u * kBlock + threadIdx.x) * V);
+#pragma unroll
+        for (int u = 0; u < kClipAsk; ++u)
+#pragma unroll
+            for (int e = 0; e < V; ++e) { const double v = (double)(float)raw[u][e]; s[u] += v * v; }
+    }
+    for (int64_t i = at + threadIdx.x * V; i < count; i += kBlock * V) {
+        const typename VecOf<T>::type raw = load_vec(p + i, i + V <= count, (int)min(count - i, (int64_t)V));
+#pragma unroll
+        for (int e = 0; e < V; ++e) { const double v = (double)(float)raw[e]; s[0] += v * v; }
+    }
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// Squares are taken and added up in 64 bits: the square of an fp32 gradient above 2e19 is no fp32 number.
+// Bound by reading.  Squares are taken and added up in 64 bits: the square of an fp32 gradient above 2e19 is no fp32 number.
 __global__ __launch_bounds__(kBlock) void clip_sums_kernel(ClipArgs a, double *__restrict__ partial) {
     __shared__ double lds[kBlock / kWave];
     const int t = clip_tensor(a, blockIdx.x);
@@ -64,15 +85,45 @@ __global__ __launch_bounds__(kBlock) void clip_sums_kernel(ClipArgs a, double *_
     if (threadIdx.x == 0) partial[a.partial_at + blockIdx.x] = sum;
 }
 
+// Last piece first: the end of every unit was read last and is still in the caches.
 template <typename T>
 __device__ __forceinline__ void scale_unit(const T *p, T *out, int64_t count, float c) {
-    for (int64_t i = threadIdx.x; i < count; i += kBlock) out[i] = (T)((float)p[i] * c);
+    constexpr int V = kVec<T>;
+    int64_t at = count / kClipPiece<T> * kClipPiece<T>;
+    for (int64_t i = at + threadIdx.x * V; i < count; i += kBlock * V) {
+        const int have = (int)min(count - i, (int64_t)V);
+        const typename VecOf<T>::type raw = load_vec(p + i, have == V, have);
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = (float)raw[e] * c;
+        store_vec(out + i, have, v);
+    }
+    while (at > 0) {
+        at -= kClipPiece<T>;
+        typename VecOf<T>::type raw[kClipAsk];
+#pragma unroll
+        for (int u = 0; u < kClipAsk; ++u) raw[u] = load_vec(p + at + (u * kBlock + threadIdx.x) * V);
+#pragma unroll
+        for (int u = 0; u < kClipAsk; ++u) {
+            float v[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = (float)raw[u][e] * c;
+            store_vec(out + at + (u * kBlock + threadIdx.x) * V, V, v);
+        }
+    }
 }
 
+// Every workgroup adds up all partial sums itself, in one order, rather than wait for one more launch.
 __global__ __launch_bounds__(kBlock) void clip_scale_kernel(ClipArgs a, const double *__restrict__ partial, double max_norm, float *__restrict__ norm) {
     __shared__ double lds[kBlock / kWave];
     double s = 0.;
-    for (int i = threadIdx.x; i < a.partials; i += kBlock) s += partial[i];
+    for (int i = threadIdx.x; i < a.partials; i += 8 * kBlock) {
+        double v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = partial[min(i + u * kBlock, a.partials - 1)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += i + u * kBlock < a.partials ? v[u] : 0.;
+    }
     const double total = sqrt(block_sum64(s, lds));
     const float c = total <= max_norm ? 1.f : (float)(max_norm / total);   // (a NaN: NaN; an infinite norm: 0, and NaN for the infinite elements)
     if (blockIdx.x == 0 && a.partial_at == 0 && threadIdx.x == 0) *norm = (float)total;
@@ -107,7 +158,7 @@ int hag_clip_gradients(int64_t tensors, const hag_tensor_t *list, double max_nor
         if (t.count > 0 && (!t.in || !t.out)) { set_error("NULL pointer"); return HAG_EINVAL; }
         total += t.count;
     }
-    const int64_t unit = std::max<int64_t>(4096, (total + kClipUnits - 1) / kClipUnits);
+    const int64_t unit = std::max<int64_t>(1, (total + kClipUnits * kClipRound - 1) / (kClipUnits * kClipRound)) * kClipRound;
     // the launches' argument blocks one after the other, first to add up, then to scale
     hipStream_t s = (hipStream_t)stream;
     int64_t partials = 0;

@@ -78,12 +78,14 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int64_t i) {
 
 // lanes whose digit is this lane's, among those of `active`
 __device__ __forceinline__ uint64_t equal_digits(uint32_t digit, int bits, uint64_t active) {
+    uint32_t lo = (uint32_t)active, hi = (uint32_t)(active >> 32);
     for (int b = 0; b < bits; ++b) {
-        const bool set = digit >> b & 1;
-        const uint64_t with = __ballot(set);
-        active &= set ? with : ~with;
+        const uint32_t set = (uint32_t)((int32_t)(digit << (31 - b)) >> 31);       // all bits of it are bit b
+        const uint64_t with = __ballot(set != 0);
+        lo &= ~((uint32_t)with ^ set);
+        hi &= ~((uint32_t)(with >> 32) ^ set);
     }
-    return active;
+    return (uint64_t)hi << 32 | lo;
 }
 
 // sum over the threads before this one; all threads of the workgroup take part
@@ -159,12 +161,12 @@ __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
     } else {
         const int slices = kSortBlock >> a.bits, digit = mine & (digits - 1);
         uint32_t all = 0, before = 0;
-        for (int p0 = mine >> a.bits; p0 < a.pieces; p0 += 16 * slices) {
-            uint32_t v[16];
+        for (int p0 = mine >> a.bits; p0 < a.pieces; p0 += 32 * slices) {
+            uint32_t v[32];
 #pragma unroll
-            for (int u = 0; u < 16; ++u) v[u] = a.counts[(int64_t)min(p0 + u * slices, a.pieces - 1) * digits + digit];
+            for (int u = 0; u < 32; ++u) v[u] = a.counts[(int64_t)min(p0 + u * slices, a.pieces - 1) * digits + digit];
 #pragma unroll
-            for (int u = 0; u < 16; ++u) {
+            for (int u = 0; u < 32; ++u) {
                 const int p = p0 + u * slices;
                 all += p < a.pieces ? v[u] : 0;
                 before += p < (int)blockIdx.x ? v[u] : 0;
@@ -446,7 +448,7 @@ __global__ __launch_bounds__(kBlock) void embed_join_kernel(GradArgs a) {
 // ------------------------------------------------------------------------------------------------------------------ few tokens
 
 // Up to kFew tokens: one launch.  A workgroup looks through all ids for those of its 32 rows, sorts them by row in LDS and adds up their runs, which are whole.
-constexpr int kFew = 1024, kFewRows = 32, kFewRounds = kFew / kBlock;
+constexpr int kFew = 2048, kFewRows = 32, kFewRounds = kFew / kBlock;
 template <typename T, typename O, typename I, int LPR, bool TAIL>
 __global__ __launch_bounds__(kBlock) void embed_few_kernel(GradArgs a, const I *ids, int64_t padding) {
     constexpr int V = kVec<T>, G = kBlock / LPR, kWaves = kBlock / kWave;
