@@ -528,11 +528,10 @@ def _ids(ids, device):
 def embedding(table, ids, scale=1.0, padding=None):
     """scale * table[ids] [*ids.shape, d] of a table [rows, d] (hag_embedding).  Ids equal to `padding` (any number, a row or not) give rows of zeros, ids that are
     no row of the table rows of NaN."""
-    import torch
     device = _device()
     code, stride = _rows("table", table, device)
     id_code, (rows, d) = _ids(ids, device), table.shape
-    y = torch.empty((*ids.shape, d), dtype=table.dtype, device=table.device)
+    y = table.new_empty((*ids.shape, d))
     rc = lib().hag_embedding(ids.numel(), rows, d, code, table.data_ptr(), stride, id_code, ids.data_ptr(), HAG_NO_PADDING if padding is None else int(padding), scale,
                              y.data_ptr(), _raw_stream())
     if rc != 0:
@@ -543,42 +542,42 @@ def embedding(table, ids, scale=1.0, padding=None):
 def embedding_grad(g_y, ids, rows, scale=1.0, padding=None, dtype=None):
     """Gradient [rows, d] at the table of embedding(table, ids, scale, padding), for the gradient g_y [n, d] at its rows, n = ids.numel() (hag_embedding_grad);
     dtype: that of g_y (the default) or float32."""
-    import torch
     device = _device()
     code, stride = _rows("g_y", g_y, device)
     id_code, (n, d) = _ids(ids, device), g_y.shape
     if ids.numel() != n:
         raise ValueError(f"g_y has {n} rows for {ids.numel()} ids")
-    if dtype is None:
-        dtype = g_y.dtype
-    elif dtype not in _elements:
+    if dtype is not None and dtype not in _elements:
         raise ValueError(f"unsupported dtype {dtype}")
     if rows < 0:
         raise ValueError("rows must not be negative")
-    out = torch.empty((rows, d), dtype=dtype, device=g_y.device)
+    out = g_y.new_empty((rows, d), dtype=dtype)
     L = lib()
-    ws = torch.empty(L.hag_embedding_grad_workspace_bytes(n, rows, d), dtype=torch.uint8, device=g_y.device)
-    rc = L.hag_embedding_grad(n, rows, d, code, g_y.data_ptr(), stride, id_code, ids.data_ptr(), HAG_NO_PADDING if padding is None else int(padding), scale, _elements[dtype],
-                              out.data_ptr(), ws.data_ptr(), _raw_stream())
+    ws = g_y.new_empty(_elements_of(L.hag_embedding_grad_workspace_bytes(n, rows, d), code))
+    rc = L.hag_embedding_grad(n, rows, d, code, g_y.data_ptr(), stride, id_code, ids.data_ptr(), HAG_NO_PADDING if padding is None else int(padding), scale,
+                              code if dtype is None else _elements[dtype], out.data_ptr(), ws.data_ptr(), _raw_stream())
     if rc != 0:
         _check(rc)
     return out
 
 
+def _elements_of(nbytes, code):
+    """Elements of the type that take so many bytes: a workspace made as a tensor like the call's own takes half as long to make as one of bytes."""
+    return nbytes // 4 if code == HAG_F32 else nbytes // 2
+
+
 def _norm_params(x, weight, bias):
     """The element code of weight and bias, which have the type of x or are float32, and their addresses."""
-    code, ptrs = None, []
-    for name, t in (("weight", weight), ("bias", bias)):
+    code, ptrs, d = None, [None, None], x.shape[1]
+    for k, t in enumerate((weight, bias)):
         if t is None:
-            ptrs.append(None)
             continue
         got = _elements.get(t.dtype)
-        if t.dim() != 1 or t.shape[0] != x.shape[1] or t.get_device() != x.get_device() or not t.is_contiguous() or code not in (None, got) \
-                or (got != HAG_F32 and t.dtype != x.dtype):
-            raise ValueError(f"{name} must have one contiguous element for each of the {x.shape[1]} columns, float32 or of the type of x, on its device; got {t.dtype} "
-                             f"{tuple(t.shape)} on {t.device}")
+        if t.shape != (d,) or t.get_device() != x.get_device() or not t.is_contiguous() or (got != HAG_F32 and t.dtype != x.dtype) or (code is not None and got != code):
+            raise ValueError(f"{('weight', 'bias')[k]} must have one contiguous element for each of the {d} columns, float32 or of the type of x, on its device (and both the "
+                             f"same); got {t.dtype} {tuple(t.shape)} on {t.device}")
         code = got
-        ptrs.append(t.data_ptr())
+        ptrs[k] = t.data_ptr()
     return HAG_F32 if code is None else code, ptrs
 
 
@@ -588,8 +587,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
     code, stride = _rows("x", x, _device())
     n, d = x.shape
     param_code, (w, b) = _norm_params(x, weight, bias)
-    y = torch.empty((n, d), dtype=x.dtype, device=x.device)
-    mean, rstd = torch.empty(n, dtype=torch.float32, device=x.device), torch.empty(n, dtype=torch.float32, device=x.device)
+    f32 = None if code == HAG_F32 else torch.float32       # (of x, or)
+    y, mean, rstd = x.new_empty((n, d)), x.new_empty(n, dtype=f32), x.new_empty(n, dtype=f32)
     rc = lib().hag_layer_norm(n, d, code, x.data_ptr(), stride, param_code, w, b, eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _raw_stream())
     if rc != 0:
         _check(rc)
@@ -599,7 +598,6 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
 def layer_norm_grad(g_y, x, mean, rstd, weight=None, params=True):
     """(g_x, g_weight, g_bias): the gradients of layer_norm for the gradient g_y at y, mean and rstd as it returned them; the latter two of the type of weight
     (float32 without one), None if not params (hag_layer_norm_grad)."""
-    import torch
     device = _device()
     code, stride = _rows("x", x, device)
     g_code, g_stride = _rows("g_y", g_y, device)
@@ -607,16 +605,16 @@ def layer_norm_grad(g_y, x, mean, rstd, weight=None, params=True):
         raise ValueError(f"g_y must match x: {x.dtype} {tuple(x.shape)}, got {g_y.dtype} {tuple(g_y.shape)}")
     n, d = x.shape
     for name, t in (("mean", mean), ("rstd", rstd)):
-        if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or t.get_device() != device or not t.is_contiguous():
+        if _elements.get(t.dtype) != HAG_F32 or t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous float32, one for each of the {n} rows, on the current device")
     param_code, (w, _) = _norm_params(x, weight, None)
-    g_x, g_w, g_b, ws = torch.empty((n, d), dtype=x.dtype, device=x.device), None, None, None
+    g_x, g_w, g_b, where = x.new_empty((n, d)), None, None, (None, None, None)
     L = lib()
     if params:
-        g_w, g_b = (torch.empty(d, dtype=torch.float32 if weight is None else weight.dtype, device=x.device) for _ in range(2))
-        ws = torch.empty(L.hag_layer_norm_grad_workspace_bytes(n, d), dtype=torch.uint8, device=x.device)
-    rc = L.hag_layer_norm_grad(n, d, code, g_y.data_ptr(), g_stride, x.data_ptr(), stride, param_code, w, mean.data_ptr(), rstd.data_ptr(), g_x.data_ptr(),
-                               *((g_w.data_ptr(), g_b.data_ptr(), ws.data_ptr()) if params else (None, None, None)), _raw_stream())
+        like = mean if weight is None else weight
+        g_w, g_b, ws = like.new_empty(d), like.new_empty(d), mean.new_empty(L.hag_layer_norm_grad_workspace_bytes(n, d) // 4)
+        where = g_w.data_ptr(), g_b.data_ptr(), ws.data_ptr()
+    rc = L.hag_layer_norm_grad(n, d, code, g_y.data_ptr(), g_stride, x.data_ptr(), stride, param_code, w, mean.data_ptr(), rstd.data_ptr(), g_x.data_ptr(), *where, _raw_stream())
     if rc != 0:
         _check(rc)
     return g_x, g_w, g_b
@@ -624,8 +622,6 @@ def layer_norm_grad(g_y, x, mean, rstd, weight=None, params=True):
 
 def _dense(t):
     """Its elements fill a piece of memory, in whatever order of the dimensions."""
-    if t.is_contiguous():
-        return True
     count = 1
     for stride, size in sorted((stride, size) for stride, size in zip(t.stride(), t.shape) if size != 1):
         if stride != count:
@@ -643,23 +639,25 @@ def clip_gradients(tensors, max_norm, out=None):
     if len(outs) != len(tensors):
         raise ValueError(f"{len(outs)} outputs for {len(tensors)} tensors")
     device, codes = _device(), _elements or _element_codes()
-    entries = array.array("q")
+    entries = []
     for t, o in zip(tensors, outs):
-        code = codes.get(t.dtype)
-        if code is None or t.get_device() != device or not _dense(t):
+        code, whole = codes.get(t.dtype), t.is_contiguous()
+        if code is None or t.get_device() != device or not (whole or _dense(t)):
             raise ValueError(f"dense float32, bfloat16 or float16 tensors on the current device are needed, got {t.dtype} {tuple(t.shape)} with strides {tuple(t.stride())} on {t.device}")
-        if o is not t and (o.dtype != t.dtype or o.shape != t.shape or o.get_device() != device or o.stride() != t.stride()):
+        if o is not t and (o.dtype != t.dtype or o.shape != t.shape or o.get_device() != device or not (whole and o.is_contiguous() or o.stride() == t.stride())):
             raise ValueError(f"an output must match its tensor: {t.dtype} {tuple(t.shape)} with strides {tuple(t.stride())}, got {o.dtype} {tuple(o.shape)} with {tuple(o.stride())}")
         count = t.numel()
         if count:
-            entries.extend((t.data_ptr(), o.data_ptr(), count, code))
+            at = t.data_ptr()
+            entries += (at, at if o is t else o.data_ptr(), count, code)
     count = len(entries) // 4
     if len(set(entries[1::4])) != count:
         raise ValueError("a tensor is named twice")
-    norm = torch.empty((), dtype=torch.float32, device="cuda")
     L = lib()
     ws = torch.empty(L.hag_clip_workspace_bytes(count), dtype=torch.uint8, device="cuda")
-    rc = L.hag_clip_gradients(count, entries.buffer_info()[0], max_norm, norm.data_ptr(), ws.data_ptr(), _raw_stream())
+    norm = torch.empty((), dtype=torch.float32, device="cuda")
+    table = array.array("q", entries)
+    rc = L.hag_clip_gradients(count, table.buffer_info()[0], max_norm, norm.data_ptr(), ws.data_ptr(), _raw_stream())
     if rc != 0:
         _check(rc)
     return norm

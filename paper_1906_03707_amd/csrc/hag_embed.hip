@@ -60,11 +60,12 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
 // counts per piece of the list, then every piece finds where each of its digits begins (the counts of smaller digits and of earlier pieces) and writes its tokens there.
 // Few bytes, so what it costs is the way of a piece through the steps of a pass: many loads at a time, few pieces to look back at.
 constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / kWave, kSortRounds = 4, kSortTile = kSortBlock * kSortRounds, kSortBits = 10, kSortPieces = 128;
+constexpr int kSortGroup = 2;        // pieces that are counted together
 constexpr int kSortAlone = 4;        // so few pieces count the others' tokens themselves
 struct SortArgs {
     const void *ids;                 // first pass: the tokens' ids
     const uint32_t *keys, *tokens;   // later passes: what the one before wrote
-    uint32_t *keys_out, *tokens_out, *counts;
+    uint32_t *keys_out, *tokens_out, *counts, *group_counts;
     int64_t n, rows, padding, piece; // tokens of a piece, a multiple of kSortTile
     int32_t pieces, shift, bits;
 };
@@ -79,24 +80,31 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int64_t i) {
 // lanes whose digit is this lane's, among those of `active`
 __device__ __forceinline__ uint64_t equal_digits(uint32_t digit, int bits, uint64_t active) {
     uint32_t lo = (uint32_t)active, hi = (uint32_t)(active >> 32);
-    for (int b = 0; b < bits; ++b) {
-        const uint32_t set = (uint32_t)((int32_t)(digit << (31 - b)) >> 31);       // all bits of it are bit b
-        const uint64_t with = __ballot(set != 0);
-        lo &= ~((uint32_t)with ^ set);
-        hi &= ~((uint32_t)(with >> 32) ^ set);
+#pragma unroll
+    for (int b = 0; b < kSortBits; ++b) {
+        if (b < bits) {
+            const uint32_t set = (uint32_t)((int32_t)(digit << (31 - b)) >> 31);   // all bits of it are bit b
+            const uint64_t with = __ballot(set != 0);
+            lo &= ~((uint32_t)with ^ set);
+            hi &= ~((uint32_t)(with >> 32) ^ set);
+        }
     }
     return (uint64_t)hi << 32 | lo;
 }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_zero(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
+
 // sum over the threads before this one; all threads of the workgroup take part
 __device__ __forceinline__ uint32_t threads_before(uint32_t v, uint32_t *wave_sum) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    uint32_t sum = v;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const uint32_t u = __shfl_up(sum, off);
-        sum += lane >= off ? u : 0;
-    }
+    uint32_t sum = v;                                      // of the lanes up to this one: shifts within rows of 16, then the last lanes of rows and of halves
+    sum += dpp_or_zero<0x111, 0xf>(sum);
+    sum += dpp_or_zero<0x112, 0xf>(sum);
+    sum += dpp_or_zero<0x114, 0xf>(sum);
+    sum += dpp_or_zero<0x118, 0xf>(sum);
+    sum += dpp_or_zero<0x142, 0xa>(sum);
+    sum += dpp_or_zero<0x143, 0xc>(sum);
     if (lane == kWave - 1) wave_sum[wave] = sum;
     __syncthreads();
     uint32_t before = 0;
@@ -105,29 +113,48 @@ __device__ __forceinline__ uint32_t threads_before(uint32_t v, uint32_t *wave_su
     return before + sum - v;
 }
 
-// count[digit] of the tokens begin .. end
+// count[digit] of the tokens begin .. end, which `threads` threads share.  The lanes that have the first lane's digit add once: an id that is named most of the time would
+// have all 64 wait for each other (370000 tokens of one id: 12 us, so 7).
 template <typename I, bool FIRST>
-__device__ __forceinline__ void count_digits(const SortArgs &a, int64_t begin, int64_t end, uint32_t *count) {
-    for (int64_t tile = begin; tile < end; tile += kSortTile) {
-        uint32_t key[kSortRounds];
+__device__ __forceinline__ void count_digits(const SortArgs &a, int64_t begin, int64_t end, int thread, int threads, uint32_t *count) {
+    constexpr int kAsk = 8;
+    for (int64_t at = begin + thread; at < end; at += kAsk * threads) {
+        uint32_t key[kAsk];
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r) key[r] = sort_key<I, FIRST>(a, min(tile + r * kSortBlock + threadIdx.x, end - 1));
+        for (int r = 0; r < kAsk; ++r) key[r] = sort_key<I, FIRST>(a, min(at + r * threads, end - 1));
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r)
-            if (tile + r * kSortBlock + threadIdx.x < end) atomicAdd(&count[key[r] >> a.shift & ((1u << a.bits) - 1)], 1u);
+        for (int r = 0; r < kAsk; ++r) {
+            if (at + r * threads >= end) continue;
+            const uint32_t digit = key[r] >> a.shift & ((1u << a.bits) - 1), first = __builtin_amdgcn_readfirstlane(digit);
+            const uint64_t same = __ballot(digit == first);
+            if (digit != first) atomicAdd(&count[digit], 1u);
+            else if ((int)(threadIdx.x % kWave) == __builtin_ctzll(same)) atomicAdd(&count[digit], (uint32_t)__popcll(same));
+        }
     }
 }
 
+// A workgroup counts a group of pieces, some wavefronts each: `counts` gets the tokens of every digit in the earlier pieces of the group, `group_counts` those of the group.
 template <typename I, bool FIRST>
 __global__ __launch_bounds__(kSortBlock) void sort_count_kernel(SortArgs a) {
-    __shared__ uint32_t count[1 << kSortBits];
-    const int digits = 1 << a.bits;
-    if ((int)threadIdx.x < digits) count[threadIdx.x] = 0;
+    __shared__ uint32_t count[kSortGroup][1 << kSortBits];
+    constexpr int kThreads = kSortBlock / kSortGroup;
+    const int digits = 1 << a.bits, mine = threadIdx.x, k = mine / kThreads;
+    if (mine < digits)
+#pragma unroll
+        for (int q = 0; q < kSortGroup; ++q) count[q][mine] = 0;
     __syncthreads();
-    const int64_t begin = (int64_t)blockIdx.x * a.piece;
-    count_digits<I, FIRST>(a, begin, min(begin + a.piece, a.n), count);
+    const int64_t begin = ((int64_t)blockIdx.x * kSortGroup + k) * a.piece;
+    count_digits<I, FIRST>(a, begin, min(begin + a.piece, a.n), mine % kThreads, kThreads, count[k]);
     __syncthreads();
-    if ((int)threadIdx.x < digits) a.counts[(int64_t)blockIdx.x * digits + threadIdx.x] = count[threadIdx.x];
+    if (mine >= digits) return;
+    uint32_t sum = 0;
+#pragma unroll
+    for (int q = 0; q < kSortGroup; ++q) {
+        const int p = blockIdx.x * kSortGroup + q;
+        if (p < a.pieces) a.counts[(int64_t)p * digits + mine] = sum;
+        sum += count[q][mine];
+    }
+    a.group_counts[(int64_t)blockIdx.x * digits + mine] = sum;
 }
 
 // Within a tile a wavefront takes 256 tokens in their order, 64 at a time; a token's place in the tile is where its digit begins, plus the tokens of that digit in earlier wavefronts, in
@@ -154,22 +181,22 @@ __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
     __syncthreads();
     // total: tokens of every digit; base: those of earlier pieces
     if (a.pieces <= kSortAlone) {
-        count_digits<I, FIRST>(a, 0, begin, base);
-        count_digits<I, FIRST>(a, begin, a.n, total);
+        count_digits<I, FIRST>(a, 0, begin, mine, kSortBlock, base);
+        count_digits<I, FIRST>(a, begin, a.n, mine, kSortBlock, total);
         __syncthreads();
         if (mine < digits) total[mine] += base[mine];
     } else {
-        const int slices = kSortBlock >> a.bits, digit = mine & (digits - 1);
-        uint32_t all = 0, before = 0;
-        for (int p0 = mine >> a.bits; p0 < a.pieces; p0 += 32 * slices) {
+        const int slices = kSortBlock >> a.bits, digit = mine & (digits - 1), groups = (a.pieces + kSortGroup - 1) / kSortGroup, own = (int)blockIdx.x / kSortGroup;
+        uint32_t all = 0, before = mine < digits ? a.counts[(int64_t)blockIdx.x * digits + mine] : 0;
+        for (int g0 = mine >> a.bits; g0 < groups; g0 += 32 * slices) {
             uint32_t v[32];
 #pragma unroll
-            for (int u = 0; u < 32; ++u) v[u] = a.counts[(int64_t)min(p0 + u * slices, a.pieces - 1) * digits + digit];
+            for (int u = 0; u < 32; ++u) v[u] = a.group_counts[(int64_t)min(g0 + u * slices, groups - 1) * digits + digit];
 #pragma unroll
             for (int u = 0; u < 32; ++u) {
-                const int p = p0 + u * slices;
-                all += p < a.pieces ? v[u] : 0;
-                before += p < (int)blockIdx.x ? v[u] : 0;
+                const int g = g0 + u * slices;
+                all += g < groups ? v[u] : 0;
+                before += g < own ? v[u] : 0;
             }
         }
         atomicAdd(&total[digit], all);
@@ -185,16 +212,19 @@ __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
         for (int c = mine; c < (kSortWaves << a.bits) / 2; c += kSortBlock) space[c] = 0;
         __syncthreads();
         uint32_t place[kSortRounds];
+        uint64_t same[kSortRounds];                        // lanes of the same digit
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r) {
-            const bool here = tile + (wave * kSortRounds + r) * kWave + lane < end;
-            const uint32_t digit = key[r] >> a.shift & (digits - 1), at = (uint32_t)wave << a.bits | digit;
-            const uint64_t same = equal_digits(digit, a.bits, __ballot(here));
-            const int leader = same ? __builtin_ctzll(same) : lane;
-            uint32_t before = 0;
-            if (here && lane == leader) before = atomicAdd(&space[at >> 1], (uint32_t)__popcll(same) << (at & 1) * 16) >> (at & 1) * 16 & 0xffff;
-            place[r] = __shfl(before, leader) + __popcll(same & ((1ull << lane) - 1));
+        for (int r = 0; r < kSortRounds; ++r)
+            same[r] = equal_digits(key[r] >> a.shift & (digits - 1), a.bits, __ballot(tile + (wave * kSortRounds + r) * kWave + lane < end));
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r) {            // the first of them adds them all to the wavefront's count
+            const uint32_t at = (uint32_t)wave << a.bits | (key[r] >> a.shift & (digits - 1));
+            place[r] = 0;
+            if (same[r] && lane == __builtin_ctzll(same[r])) place[r] = atomicAdd(&space[at >> 1], (uint32_t)__popcll(same[r]) << (at & 1) * 16) >> (at & 1) * 16 & 0xffff;
         }
+#pragma unroll
+        for (int r = 0; r < kSortRounds; ++r)
+            place[r] = __shfl(place[r], same[r] ? __builtin_ctzll(same[r]) : lane) + __popcll(same[r] & ((1ull << lane) - 1));
         __syncthreads();
         uint32_t here = 0;                                 // the tile's tokens of digit `mine`
         if (mine < digits) {
@@ -572,7 +602,7 @@ static GradPlan grad_plan(int64_t n, int64_t rows, int64_t d, int vec) {
     p.groups = (int32_t)((n + side * p.each - 1) / (side * p.each));
     auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += (bytes + 255) / 256 * 256; return at; };
     p.lists = take((size_t)n * 4 * 4);
-    p.counts = take((size_t)p.pieces * 4 << p.bits);
+    p.counts = take((size_t)(p.pieces + (p.pieces + kSortGroup - 1) / kSortGroup) * 4 << p.bits);
     p.where = take((size_t)rows * 4);
     p.part = take((size_t)p.groups * 2 * d * 4);
     return p;
@@ -665,6 +695,7 @@ int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, co
     SortArgs sort = {};
     sort.ids = ids;
     sort.counts = (uint32_t *)(ws + p.counts);
+    sort.group_counts = sort.counts + ((size_t)p.pieces << p.bits);
     sort.n = n;
     sort.rows = rows;
     sort.padding = padding;
@@ -680,7 +711,7 @@ int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, co
         typedef void (*kernel_t)(SortArgs);
         const kernel_t count = pass > 0 ? (kernel_t)sort_count_kernel<int32_t, false> : id_type == HAG_I64 ? (kernel_t)sort_count_kernel<int64_t, true> : (kernel_t)sort_count_kernel<int32_t, true>;
         const kernel_t place = pass > 0 ? (kernel_t)sort_place_kernel<int32_t, false> : id_type == HAG_I64 ? (kernel_t)sort_place_kernel<int64_t, true> : (kernel_t)sort_place_kernel<int32_t, true>;
-        if (p.pieces > kSortAlone) hipLaunchKernelGGL(count, dim3((unsigned)p.pieces), dim3(kSortBlock), 0, s, sort);
+        if (p.pieces > kSortAlone) hipLaunchKernelGGL(count, dim3((unsigned)((p.pieces + kSortGroup - 1) / kSortGroup)), dim3(kSortBlock), 0, s, sort);
         HIP_TRY(hipGetLastError());
         hipLaunchKernelGGL(place, dim3((unsigned)p.pieces), dim3(kSortBlock), 0, s, sort);
         HIP_TRY(hipGetLastError());
