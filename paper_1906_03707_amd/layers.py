@@ -1,8 +1,8 @@
 """The two GNN layers of the paper's Table 1 around the library's aggregation calls.
 
-The aggregation (and, for GCN, the normalisation fused into it), the gradients of the weight matrices
-and the SoftMax loss are this library's kernels; the other dense parts (products with the weight
-matrices, ReLU) are plain torch.  Each aggregation call can be recorded (its input and
+The aggregation (and, for GCN, the normalisation fused into it), the gradients of the weight matrices,
+the SoftMax loss, lookups of nodes' rows in a table, layer norm and the clipping of gradients are this library's
+kernels; the other dense parts (products with the weight matrices, ReLU) are plain torch.  Each aggregation call can be recorded (its input and
 output tensors), so that a test can hand exactly those inputs to the CPU oracle.
 
 GCN (Table 1, GCN row; the model of Section 5.3):  h'_v = relu(W . (a_v + h_v) / (|N(v)| + 1)) with
@@ -90,6 +90,67 @@ def softmax_loss(z, labels):
     if _plain(z) and _plain_labels(labels, z) and 0 < z.shape[1] <= 1 << 20 and z.numel() >= 1 << 19 and not torch.is_autocast_enabled() and _no_tangent(z):
         return _SoftmaxLoss.apply(z, labels)
     return torch.nn.functional.cross_entropy(z, labels)
+
+
+def _rows_of(t):
+    """t as a matrix of its last dimension whose rows are contiguous."""
+    t = t.reshape(-1, t.shape[-1]) if t.dim() != 2 else t
+    return t if t.shape[1] <= 1 or t.stride(1) == 1 else t.contiguous()
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, scale, padding):
+        ctx.save_for_backward(ids)
+        ctx.rows, ctx.scale, ctx.padding = table.shape[0], scale, padding
+        return binding.embedding(table, ids, scale, padding)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        ids, = ctx.saved_tensors
+        return binding.embedding_grad(_rows_of(g), ids, ctx.rows, ctx.scale, ctx.padding), None, None, None
+
+
+def embedding(table, ids, scale=1.0, padding=None):
+    """scale * table[ids], [*ids.shape, d]: rows for nodes that carry an id or a category (a degree, a label) instead of features.  table [rows, d] float32, bfloat16
+    or float16, ids contiguous int64 or int32.  Ids equal to `padding` give rows of zeros and send no gradient; ids that are no row of the table give rows of
+    NaN and send none.  The table's gradient is dense, added up in a fixed order; its backward pass is not itself differentiable."""
+    return _Embedding.apply(table, ids, scale, padding)
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        rows = _rows_of(x)
+        y, mean, rstd = binding.layer_norm(rows, weight, bias, eps)
+        ctx.save_for_backward(rows, weight, mean, rstd)
+        ctx.shape = x.shape
+        return y.view(x.shape)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        rows, weight, mean, rstd = ctx.saved_tensors
+        need_w, need_b = ctx.needs_input_grad[1:3]
+        g_x, g_w, g_b = binding.layer_norm_grad(_rows_of(g), rows, mean, rstd, weight, params=need_w or need_b)
+        return g_x.view(ctx.shape), g_w if need_w else None, g_b if need_b else None, None
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """Layer norm over the last dimension of x (float32, bfloat16 or float16): (x - mean) / sqrt(variance + eps) * weight + bias, weight and bias [d] of the type of x or
+    float32.  Sums over neighbours grow with the degree; normed rows keep what comes next in range.  Its backward pass is not itself differentiable."""
+    return _LayerNorm.apply(x, weight, bias, eps)
+
+
+def clip_gradients(parameters, max_norm):
+    """Scales the gradients of `parameters` (those that have one) down, in place, so that their 2-norm, taken as one vector, is at most max_norm.  The norm they had, a float32
+    scalar on the device: nothing waits for it.  An infinite norm leaves zeros and NaN, a NaN all NaN, so look at it before the parameters are changed where that can happen."""
+    grads = [p.grad for p in parameters if p.grad is not None]
+    norm = binding.clip_gradients(grads, max_norm)
+    if grads:
+        torch.autograd.graph.increment_version(grads)
+    return norm
 
 
 def aggregation(h, op, naive=False, record=None):
@@ -182,6 +243,26 @@ def gcn2_loss(h, x, w1, w2, labels, naive=False, record=None):
             and w1.shape[1] == w2.shape[0] and _narrow(*w1.shape) and _narrow(*w2.shape) and not torch.is_autocast_enabled()):
         return _Gcn2Loss.apply(x, w1, w2, labels, h, naive)
     return _gcn2_composed(h, x, w1, w2, labels, naive, record)
+
+
+def embedded_gcn2_loss(h, ids, table, norm_weight, norm_bias, w1, w2, labels, padding=None, naive=False):
+    """gcn2_loss for nodes that carry ids [n] instead of features: their rows of the table, scaled by sqrt(d) as its entries are about 1 / sqrt(d), through a layer norm."""
+    x = layer_norm(embedding(table, ids, table.shape[1] ** 0.5, padding), norm_weight, norm_bias)
+    return gcn2_loss(h, x, w1, w2, labels, naive)
+
+
+def embedded_gcn2_step(h, ids, params, labels, lr, max_norm, padding=None):
+    """One step of gradient descent on embedded_gcn2_loss with the gradients clipped to max_norm.  params: (table, norm_weight, norm_bias, w1, w2), leaves that
+    require gradients, updated in place; (loss, gradient norm), scalars on the device."""
+    for p in params:
+        p.grad = None
+    loss = embedded_gcn2_loss(h, ids, *params, labels, padding)
+    loss.backward()
+    norm = clip_gradients(params, max_norm)
+    with torch.no_grad():
+        for p in params:
+            p.sub_(p.grad, alpha=lr)
+    return loss.detach(), norm
 
 
 def sage_pool2_loss(h, x, pool, comb, labels, naive=False, record=None):
