@@ -60,9 +60,10 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
 // A token's key is its id, `rows` where it names no row: those come last and are left out.  Radix sort, low digits first, with stable passes of up to 10 bits:
 // counts per piece of the list, then every piece finds where each of its digits begins (the counts of smaller digits and of earlier pieces) and writes its tokens there.
 // Few bytes, so what it costs is the way of a piece through the steps of a pass: many loads at a time, few pieces to look back at.
-constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / kWave, kSortRounds = 4, kSortTile = kSortBlock * kSortRounds, kSortBits = 10, kSortPieces = 128;
-constexpr int kSortGroup = 2;        // pieces that are counted together
-constexpr int kSortAlone = 4;        // so few pieces count the others' tokens themselves
+constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / kWave, kSortRounds = 2, kSortTile = kSortBlock * kSortRounds, kSortBits = 10, kSortPieces = 256;
+constexpr int kSortSpace = std::max(2 * kSortTile, (kSortWaves << kSortBits) / 2);   // words
+constexpr int kSortGroup = 4;        // pieces that are counted together
+constexpr int kSortAlone = 8;        // so few pieces count the others' tokens themselves
 struct SortArgs {
     const void *ids;                 // first pass: the tokens' ids
     const uint32_t *keys, *tokens;   // later passes: what the one before wrote
@@ -158,13 +159,12 @@ __global__ __launch_bounds__(kSortBlock) void sort_count_kernel(SortArgs a) {
     a.group_counts[(int64_t)blockIdx.x * digits + mine] = sum;
 }
 
-// Within a tile a wavefront takes 256 tokens in their order, 64 at a time; a token's place in the tile is where its digit begins, plus the tokens of that digit in earlier wavefronts, in
+// Within a tile a wavefront takes 128 tokens in their order, 64 at a time; a token's place in the tile is where its digit begins, plus the tokens of that digit in earlier wavefronts, in
 // earlier rounds of its own, and in lower lanes.  The tile is put in that order in LDS first, so that neighbours are written side by side.
 template <typename I, bool FIRST>
 __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
-    __shared__ uint32_t space[2 * kSortTile];              // counts per wavefront and digit, 16 bits each; then the tile's keys and tokens in order
+    __shared__ uint32_t space[kSortSpace];                 // counts per wavefront and digit, 16 bits each; then the tile's keys and tokens in order
     __shared__ uint32_t base[1 << kSortBits], total[1 << kSortBits], wave_sum[2][kSortWaves];
-    static_assert(kSortWaves << kSortBits <= 4 * kSortTile, "counts of 16 bits in the space of the tile");
     uint16_t *count = (uint16_t *)space;
     const int digits = 1 << a.bits, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, mine = threadIdx.x;
     const int64_t begin = (int64_t)blockIdx.x * a.piece, end = min(begin + a.piece, a.n);

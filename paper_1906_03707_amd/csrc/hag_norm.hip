@@ -61,6 +61,12 @@ __device__ __forceinline__ float2 row_sums(float2 v, float2 (*lds)[16], int &tur
     return v;
 }
 
+// 1 / sqrt(v): the hardware's (one unit in the last place), and one step of Newton's method (half of one)
+__device__ __forceinline__ float inverse_root(float v) {
+    const float r = rsqrtf(v), better = fmaf(0.5f * r, fmaf(-(v * r), r, 1.f), r);
+    return r > 0.f && r < INFINITY ? better : r;           // (v infinite, zero or no number: as it is)
+}
+
 // Threads of a workgroup whose rows have LPR lanes (backward: twice as many where rows have a wavefront or less, so that there are half as many partial sums), and the rows
 // that a wavefront (or the workgroup) takes side by side.
 template <int LPR>
@@ -113,7 +119,7 @@ __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
             }
             s += col < a.d ? part : 0.f;
         }
-        r[t] = rsqrtf(row_sums<LPR>(make_float2(s, 0.f), lds, turn).x * a.inv_d + a.eps);
+        r[t] = inverse_root(row_sums<LPR>(make_float2(s, 0.f), lds, turn).x * a.inv_d + a.eps);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -334,7 +340,7 @@ __global__ __launch_bounds__(kWide) void norm_wide_kernel(NormArgs a) {
     const float m = first + wide_sum(s, lds) * a.inv_d;
     s = 0.f;
     for (int c = threadIdx.x; c < a.d; c += kWide) { const float v = (float)p[c] - m; s += v * v; }
-    const float r = rsqrtf(wide_sum(s, lds) * a.inv_d + a.eps);
+    const float r = inverse_root(wide_sum(s, lds) * a.inv_d + a.eps);
     for (int c = threadIdx.x; c < a.d; c += kWide) {
         const float xh = ((float)p[c] - m) * r;
         ((T *)a.out)[row * a.d + c] = (T)(xh * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f) + (a.bias ? param(a.bias, a.param32, T(), c) : 0.f));
