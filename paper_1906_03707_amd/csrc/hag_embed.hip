@@ -19,7 +19,8 @@ struct EmbedArgs {
 };
 
 // Bound by writing y (and by reading the table where it exceeds the caches).  LPR lanes move a row, 16 bytes each, four rows at a time: the ids first, then the rows they name.
-// Streaming stores leave the caches to the table (524288 rows of 232965, 128 columns: fp32 91 -> 85 us, bf16 43 -> 41).
+// Streaming stores leave the caches to the table (524288 rows of 232965, 128 columns: fp32 91 -> 85 us, bf16 43 -> 41).  370000 rows of 74, 64 fp32 columns: 16.3 us, 5.8 TB/s written
+// (a fill: 6.4); a call on 74 rows 7.5 us, which is the host's.
 constexpr int kEmbedRows = 4;
 template <typename T, typename I, int LPR, bool TAIL>
 __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
@@ -59,7 +60,8 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
 
 // A token's key is its id, `rows` where it names no row: those come last and are left out.  Radix sort, low digits first, with stable passes of up to 10 bits:
 // counts per piece of the list, then every piece finds where each of its digits begins (the counts of smaller digits and of earlier pieces) and writes its tokens there.
-// Few bytes, so what it costs is the way of a piece through the steps of a pass: many loads at a time, few pieces to look back at.
+// Few bytes, so what it costs is the way of a piece through the steps of a pass: many loads at a time, few pieces to look back at.  524288 tokens, 9 bits: counts 5 us, places 12; a
+// gradient with pieces of 2048 tokens 122 us, of 4096 (half of the compute units idle) 123, of 1024 (twice as many to look back at) 137.
 constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / kWave, kSortRounds = 2, kSortTile = kSortBlock * kSortRounds, kSortBits = 10, kSortPieces = 256;
 constexpr int kSortSpace = std::max(2 * kSortTile, (kSortWaves << kSortBits) / 2);   // words
 constexpr int kSortGroup = 4;        // pieces that are counted together
@@ -284,7 +286,9 @@ struct GradArgs {
 
 // Adds up runs of equal keys among `count` entries in LDS (sorted; keys[-1] is the key before them, keys[count] the one after, kNone where there is none).  Groups of LPR lanes take
 // `each` entries one after the other, requesting eight rows ahead; a run inside a group's entries is done there (store), those that cross groups go through LDS
-// (edge: [groups of lanes][LPR * V] sums of the run that began earlier and ends in the group or covers it) and are added up by the group in which they begin.  open(first, sum): a run that began before the entries (first) or goes on after them.
+// (edge: [groups of lanes][LPR * V] sums of the run that began earlier and ends in the group or covers it) and are added up by
+// the group in which they begin.  open(first, sum): a run that began before the entries (first) or goes on after them.
+// Equal pieces keep every lane busy whatever the ids are; a sum for each row of the table would last as long as the id that is named most.
 constexpr uint32_t kNone = 0xffffffffu;
 template <typename T, int LPR, bool TAIL, typename Store, typename Open>
 __device__ __forceinline__ void sum_runs(const T *gy, int64_t stride, int64_t extent, int d, int col, const uint32_t *keys, const uint32_t *tokens, int count, int each, uint32_t rows,
@@ -360,6 +364,8 @@ __device__ __forceinline__ void sum_runs(const T *gy, int64_t stride, int64_t ex
     }
 }
 
+// Bound by reading g_y in the order of the ids: 370000 x 64 fp32 into 74 rows 18 us (5.3 TB/s, what a copy moves), 524288 x 128 into 232965 rows, 512 bytes here and there, 74 to 78 us
+// (245 MB in, 105 out, 4.5 TB/s); 4 or 16 rows ahead instead of 8, 16 entries instead of 32: the same.
 constexpr int kEachMost = 32;
 template <typename T, typename O, int LPR, bool TAIL>
 __global__ __launch_bounds__(kBlock) void embed_sum_kernel(GradArgs a) {
@@ -403,6 +409,7 @@ __global__ __launch_bounds__(kBlock) void embed_sum_kernel(GradArgs a) {
         });
 }
 
+// 8 us for those 232965 rows, 4 for 74.
 // The first `groups` - 1 workgroups: the run that begins among the entries of workgroup b of the sums and goes on after them.  The others: 64 rows of g_table for each wavefront, zeros
 // where no token names them.
 template <typename T, typename O, int LPR, bool TAIL>
@@ -478,7 +485,8 @@ __global__ __launch_bounds__(kBlock) void embed_join_kernel(GradArgs a) {
 
 // ------------------------------------------------------------------------------------------------------------------ few tokens
 
-// Up to kFew tokens: one launch.  A workgroup looks through all ids for those of its 32 rows, sorts them by row in LDS and adds up their runs, which are whole.
+// Up to kFew tokens: one launch, 9 us for 777 tokens of 37 columns in 4096 rows where the path above takes 25.  (2048 tokens: 11 and 26, but 33 and 29 if all name one row; 4096: 11 and
+// 27, 67 and 33.)  A workgroup looks through all ids for those of its 32 rows, sorts them by row in LDS and adds up their runs, which are whole.
 constexpr int kFew = 2048, kFewRows = 32, kFewRounds = kFew / kBlock;
 template <typename T, typename O, typename I, int LPR, bool TAIL>
 __global__ __launch_bounds__(kBlock) void embed_few_kernel(GradArgs a, const I *ids, int64_t padding) {
@@ -492,11 +500,19 @@ __global__ __launch_bounds__(kBlock) void embed_few_kernel(GradArgs a, const I *
     for (int c = threadIdx.x; c < kWaves * kFewRows; c += kBlock) count[c / kFewRows][c % kFewRows] = 0;
     __syncthreads();
     uint32_t row[kFewRounds], rank[kFewRounds];
+    const int n = (int)a.n, rounds = (n + kBlock - 1) / kBlock;    // a wavefront takes so many times 64 tokens
+    if (n > 0) {
+        int64_t id[kFewRounds];
 #pragma unroll
-    for (int r = 0; r < kFewRounds; ++r) {
-        const int i = (wave * kFewRounds + r) * kWave + lane;
-        const int64_t id = i < a.n ? (int64_t)ids[i] : -1;
-        row[r] = id >= row0 && id < a.rows && id != padding && id - row0 < kFewRows ? (uint32_t)(id - row0) : kNone;
+        for (int r = 0; r < kFewRounds; ++r) id[r] = ids[min((wave * rounds + min(r, rounds - 1)) * kWave + lane, n - 1)];
+#pragma unroll
+        for (int r = 0; r < kFewRounds; ++r) {
+            const bool here = r < rounds && (wave * rounds + r) * kWave + lane < n;
+            row[r] = here && id[r] >= row0 && id[r] < a.rows && id[r] != padding && id[r] - row0 < kFewRows ? (uint32_t)(id[r] - row0) : kNone;
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < kFewRounds; ++r) row[r] = kNone;
     }
 #pragma unroll
     for (int r = 0; r < kFewRounds; ++r) {
@@ -538,7 +554,7 @@ __global__ __launch_bounds__(kBlock) void embed_few_kernel(GradArgs a, const I *
         if (row[r] != kNone) {
             const uint32_t to = count[wave][row[r]] + rank[r];
             keys[to] = row[r];
-            tokens[to] = (uint32_t)((wave * kFewRounds + r) * kWave + lane);
+            tokens[to] = (uint32_t)((wave * rounds + r) * kWave + lane);
         }
     const int found = (int)begins[kFewRows];
     if (threadIdx.x == 0) keys[-1] = keys[found] = kNone;

@@ -76,7 +76,8 @@ constexpr int kGradBlock = LPR <= kWave ? 2 * kBlock : LPR;
 template <int LPR>
 constexpr int kSide = LPR <= kWave ? kWave / LPR : 1;
 
-// Bound by reading x and writing y.  Every lane requests R rows one after the other before it needs the first.
+// Bound by reading x and writing y.  Every lane requests R rows one after the other before it needs the first.  232965 x 128 fp32 40 us, bf16 21 (5.9 and 5.8 TB/s; a copy: 5.3),
+// 56944 x 251 bf16, rows at any address, 15.7 (3.6).
 template <typename T, int LPR, int K, int R, bool TAIL>
 __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
     __shared__ float2 lds[2][16];
@@ -157,6 +158,7 @@ __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
 
 // Bound by reading x and g_y and writing g_x.  Workgroups take rows in turn, keep the sums of their columns for g_w and g_b in registers, and leave them in `partial`, one
 // row of 2 d for each workgroup, added up in a fixed order by norm_reduce_kernel.  The next rows are requested before the present ones are worked on.
+// 65536 x 512 fp32 78 us with the last sums (5.2 TB/s), 232965 x 128 bf16 35 (5.1), 56944 x 251 bf16 21 (4.1).
 template <typename T, int LPR, int K, int R, bool TAIL>
 __global__ __launch_bounds__(kGradBlock<LPR>) void norm_grad_kernel(NormArgs a) {
     extern __shared__ float sums[];                        // [wavefronts][2][LPR * K * V], rows of up to 64 lanes
