@@ -269,6 +269,46 @@ __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
     }
 }
 
+// Up to kRankMost tokens are put in order by one launch instead of two passes: a token's place is the number of tokens that come before it, counted by comparing it with all of them (2 vector
+// instructions for 64 pairs, and LDS for the keys: a gradient of 8192 tokens 21 us where two passes make it 25, of 16384 38 and 27).  A workgroup places 32 tokens, 16 lanes each, out of all keys in LDS.
+constexpr int kRankMost = 8192, kRankTokens = 32, kRankBlock = 512, kRankStreams = kRankBlock / kRankTokens, kRankAsk = kRankMost / kRankBlock;
+template <typename I>
+__global__ __launch_bounds__(kRankBlock) void sort_rank_kernel(SortArgs a) {
+    __shared__ uint4 keys[kRankMost / 4];
+    __shared__ uint32_t count[kRankTokens];
+    uint32_t *key = (uint32_t *)keys;
+    const int n = (int)a.n, vectors = (n + 3) / 4, first = blockIdx.x * kRankTokens, token = threadIdx.x % kRankTokens, stream = threadIdx.x / kRankTokens, i = first + token;
+    {
+        uint32_t k[kRankAsk];
+#pragma unroll
+        for (int r = 0; r < kRankAsk; ++r) k[r] = sort_key<I, true>(a, min(r * kRankBlock + (int)threadIdx.x, n - 1));
+#pragma unroll
+        for (int r = 0; r < kRankAsk; ++r)
+            if (r * kRankBlock < 4 * vectors) key[r * kRankBlock + threadIdx.x] = r * kRankBlock + (int)threadIdx.x < n ? k[r] : 0xffffffffu;
+    }
+    if (threadIdx.x < kRankTokens) count[threadIdx.x] = 0;
+    __syncthreads();
+    const uint32_t mine = i < n ? key[i] : 0;
+    uint32_t before = 0;
+#pragma unroll 4
+    for (int v = stream; v < vectors; v += kRankStreams) {
+        const uint4 k = keys[v];
+        const uint32_t limit = mine + (4 * v < first ? 1 : 0);                     // equal keys of the workgroups before this one come first
+        before += k.x < limit;
+        before += k.y < limit;
+        before += k.z < limit;
+        before += k.w < limit;
+    }
+    for (int q = stream; q < token; q += kRankStreams) before += key[first + q] == mine;                 // and those before it in its own
+    before += __shfl_xor(before, kRankTokens);
+    if (threadIdx.x % kWave < kRankTokens) atomicAdd(&count[token], before);
+    __syncthreads();
+    if (threadIdx.x < kRankTokens && i < n) {
+        a.keys_out[count[token]] = mine;
+        a.tokens_out[count[token]] = (uint32_t)i;
+    }
+}
+
 // ------------------------------------------------------------------------------------------------------------------ sums of sorted tokens
 
 struct GradArgs {
@@ -409,7 +449,7 @@ __global__ __launch_bounds__(kBlock) void embed_sum_kernel(GradArgs a) {
         });
 }
 
-// 8 us for those 232965 rows, 4 for 74.
+// 8 us for those 232965 rows, 4 for 74; 5 us for 232965 rows of 16 columns most of which are zeros.
 // The first `groups` - 1 workgroups: the run that begins among the entries of workgroup b of the sums and goes on after them.  The others: 64 rows of g_table for each wavefront, zeros
 // where no token names them.
 template <typename T, typename O, int LPR, bool TAIL>
@@ -472,6 +512,12 @@ __global__ __launch_bounds__(kBlock) void embed_join_kernel(GradArgs a) {
     }
     const float zero[V] = {};
     uint64_t rest = __ballot(empty);
+    if (!TAIL && __popcll(rest) >= kWave / 2) {           // most of the rows: as one piece of memory, without the vectors of rows that are named
+        O *p = (O *)a.out + row0 * a.d;
+        for (uint32_t c = lane * V; c < (uint32_t)(kWave * a.d) && rest; c += kWave * V)
+            if (rest >> (c / (uint32_t)a.d) & 1) store_cols(p + c, V, zero);
+        return;
+    }
     for (; rest; ) {                                       // kWave / LPR of them at a time
         uint64_t mine = rest;
         for (int k = 0; k < lane / LPR; ++k) mine &= mine - 1;
@@ -719,7 +765,15 @@ int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, co
     sort.piece = p.piece;
     sort.pieces = p.pieces;
     sort.bits = p.bits;
-    for (int pass = 0; pass < p.passes; ++pass) {
+    if (n <= kRankMost) {
+        sort.keys_out = lists;
+        sort.tokens_out = lists + n;
+        const dim3 grid((unsigned)((n + kRankTokens - 1) / kRankTokens));
+        if (id_type == HAG_I64) hipLaunchKernelGGL(sort_rank_kernel<int64_t>, grid, dim3(kRankBlock), 0, s, sort);
+        else hipLaunchKernelGGL(sort_rank_kernel<int32_t>, grid, dim3(kRankBlock), 0, s, sort);
+        HIP_TRY(hipGetLastError());
+    }
+    for (int pass = 0; n > kRankMost && pass < p.passes; ++pass) {
         sort.shift = pass * p.bits;
         sort.keys = sort.keys_out;
         sort.tokens = sort.tokens_out;

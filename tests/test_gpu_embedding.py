@@ -97,7 +97,8 @@ def test_lookup_past_32_bits(B):
 @pytest.mark.parametrize("kind", ["even", "skew", "one"])
 @pytest.mark.parametrize("n,rows,d", [(1, 1, 1), (1, 700, 5), (2, 3, 64), (63, 64, 3), (64, 10, 16), (65, 7, 37), (256, 1000, 64), (257, 74, 33), (1000, 5, 130), (1025, 4096, 20),
                                       (4096, 300, 64), (4097, 40, 96), (8191, 70000, 4), (8193, 1024, 65), (16385, 1025, 8), (50000, 74, 64), (70001, 12, 31), (33000, 1 << 20, 4),
-                                      (20000, 3000001, 3), (300, 200, 1030), (5000, 100, 1025), (200001, 9000, 16)])
+                                      (20000, 3000001, 3), (300, 200, 1030), (5000, 100, 1025), (200001, 9000, 16), (2048, 33, 64), (2049, 33, 64), (8192, 3, 32), (8193, 5000, 16), (4100, 200000, 12),
+                                      (16384, 900, 20), (16385, 900, 20), (600000, 2000, 4)])
 def test_gradient(B, n, rows, d, kind):
     gen = torch.Generator(device="cuda").manual_seed(n + rows + d)
     ids = make_ids(n, rows, kind, gen)
@@ -131,6 +132,18 @@ def test_gradient_counts_every_token_once(B, n, rows, d):
     gy = torch.randint(-3, 4, (n, d), device="cuda", generator=gen).float()
     want = torch.zeros(rows, d, device="cuda", dtype=torch.float64).index_add_(0, ids, gy.double())
     assert torch.equal(B.embedding_grad(gy, ids, rows).double(), want)             # whole numbers below 2^24: exact in any order
+
+
+def test_gradient_past_32_bits(B):
+    n, rows, d = 33000, 33000, 70000                       # 2.3e9 elements on both sides
+    gy = torch.zeros(n, d, device="cuda", dtype=torch.bfloat16)
+    ids = torch.arange(n, device="cuda")
+    ids[:3], ids[-1] = rows - 1, 7
+    for i in (0, 2, n - 2, n - 1):
+        gy[i] = (torch.arange(d, device="cuda") % 50 + i % 7).bfloat16()
+    got = B.embedding_grad(gy, ids, rows)
+    assert torch.equal(got[rows - 1], gy[0] + gy[2]) and torch.equal(got[7], gy[n - 1]) and torch.equal(got[n - 2], gy[n - 2])
+    assert int(got.count_nonzero()) == sum(int(got[i].count_nonzero()) for i in (7, n - 2, rows - 1))
 
 
 def test_gradient_of_views(B):
