@@ -31,13 +31,13 @@ def make_ids(n, rows, kind, gen, dtype=torch.int64):
 
 
 def reference_grad(gy, ids, rows, scale, padding):
-    """(sum, sum of magnitudes, number of terms) in 64 bits."""
+    """(sum, sum of magnitudes, number of terms) in 64 bits, added up on the CPU."""
     kept = (ids >= 0) & (ids < rows)
     if padding is not None:
         kept &= ids != padding
-    at, g = ids[kept].long(), gy[kept].double() * scale
-    total, size = (torch.zeros(rows, gy.shape[1], device="cuda", dtype=torch.float64) for _ in range(2))
-    return total.index_add_(0, at, g), size.index_add_(0, at, g.abs()), torch.bincount(at, minlength=rows)[:, None]
+    at, g = ids[kept].long().cpu(), gy[kept].cpu().double() * scale
+    total, size = (torch.zeros(rows, gy.shape[1], dtype=torch.float64) for _ in range(2))
+    return total.index_add_(0, at, g).cuda(), size.index_add_(0, at, g.abs()).cuda(), torch.bincount(at, minlength=rows)[:, None].cuda()
 
 
 def check_grad(got, gy, ids, rows, scale, padding):
