@@ -62,15 +62,21 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
 // counts per piece of the list, then every piece finds where each of its digits begins (the counts of smaller digits and of earlier pieces) and writes its tokens there.
 // Few bytes, so what it costs is the way of a piece through the steps of a pass: many loads at a time, few pieces to look back at.  524288 tokens, 9 bits: counts 5 us, places 12; a
 // gradient with pieces of 2048 tokens 122 us, of 4096 (half of the compute units idle) 123, of 1024 (twice as many to look back at) 137.
-constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / kWave, kSortRounds = 2, kSortTile = kSortBlock * kSortRounds, kSortBits = 10, kSortPieces = 256;
-constexpr int kSortSpace = std::max(2 * kSortTile, (kSortWaves << kSortBits) / 2);   // words
-constexpr int kSortGroup = 4;        // pieces that are counted together
-constexpr int kSortAlone = 8;        // so few pieces count the others' tokens themselves
+// Up to kSortShort tokens the tiles are half as long: twice as many compute units have one (12000 tokens of 64 columns 30.5 -> 28.6 us, 30000 34.9 -> 33.5; 370000 36 -> 43).
+constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / kWave, kSortBits = 10, kSortPieces = 256;
+constexpr int64_t kSortShort = 128 * kSortBlock, kSortAlone = 16 * kSortBlock;     // (so few tokens every piece counts itself)
+template <int ROUNDS>                // of 64 tokens that a wavefront takes of a tile
+constexpr int kSortTile = kSortBlock * ROUNDS;
+template <int ROUNDS>
+constexpr int kSortGroup = 8 / ROUNDS;   // pieces that are counted together
+template <int ROUNDS>
+constexpr int kSortSpace = std::max(2 * kSortTile<ROUNDS>, (kSortWaves << kSortBits) / 2);   // words
+static int sort_rounds(int64_t n) { return n <= kSortShort ? 1 : 2; }
 struct SortArgs {
     const void *ids;                 // first pass: the tokens' ids
     const uint32_t *keys, *tokens;   // later passes: what the one before wrote
     uint32_t *keys_out, *tokens_out, *counts, *group_counts;
-    int64_t n, rows, padding, piece; // tokens of a piece, a multiple of kSortTile
+    int64_t n, rows, padding, piece; // tokens of a piece, a multiple of the tile
     int32_t pieces, shift, bits;
 };
 
@@ -138,43 +144,45 @@ __device__ __forceinline__ void count_digits(const SortArgs &a, int64_t begin, i
 }
 
 // A workgroup counts a group of pieces, some wavefronts each: `counts` gets the tokens of every digit in the earlier pieces of the group, `group_counts` those of the group.
-template <typename I, bool FIRST>
+template <typename I, bool FIRST, int ROUNDS>
 __global__ __launch_bounds__(kSortBlock) void sort_count_kernel(SortArgs a) {
-    __shared__ uint32_t count[kSortGroup][1 << kSortBits];
-    constexpr int kThreads = kSortBlock / kSortGroup;
+    constexpr int kGroup = kSortGroup<ROUNDS>;
+    __shared__ uint32_t count[kGroup][1 << kSortBits];
+    constexpr int kThreads = kSortBlock / kGroup;
     const int digits = 1 << a.bits, mine = threadIdx.x, k = mine / kThreads;
     if (mine < digits)
 #pragma unroll
-        for (int q = 0; q < kSortGroup; ++q) count[q][mine] = 0;
+        for (int q = 0; q < kGroup; ++q) count[q][mine] = 0;
     __syncthreads();
-    const int64_t begin = ((int64_t)blockIdx.x * kSortGroup + k) * a.piece;
+    const int64_t begin = ((int64_t)blockIdx.x * kGroup + k) * a.piece;
     count_digits<I, FIRST>(a, begin, min(begin + a.piece, a.n), mine % kThreads, kThreads, count[k]);
     __syncthreads();
     if (mine >= digits) return;
     uint32_t sum = 0;
 #pragma unroll
-    for (int q = 0; q < kSortGroup; ++q) {
-        const int p = blockIdx.x * kSortGroup + q;
+    for (int q = 0; q < kGroup; ++q) {
+        const int p = blockIdx.x * kGroup + q;
         if (p < a.pieces) a.counts[(int64_t)p * digits + mine] = sum;
         sum += count[q][mine];
     }
     a.group_counts[(int64_t)blockIdx.x * digits + mine] = sum;
 }
 
-// Within a tile a wavefront takes 128 tokens in their order, 64 at a time; a token's place in the tile is where its digit begins, plus the tokens of that digit in earlier wavefronts, in
+// Within a tile a wavefront takes its tokens in their order, 64 at a time; a token's place in the tile is where its digit begins, plus the tokens of that digit in earlier wavefronts, in
 // earlier rounds of its own, and in lower lanes.  The tile is put in that order in LDS first, so that neighbours are written side by side.
-template <typename I, bool FIRST>
+template <typename I, bool FIRST, int ROUNDS>
 __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
-    __shared__ uint32_t space[kSortSpace];                 // counts per wavefront and digit, 16 bits each; then the tile's keys and tokens in order
+    constexpr int kTile = kSortTile<ROUNDS>, kGroup = kSortGroup<ROUNDS>;
+    __shared__ uint32_t space[kSortSpace<ROUNDS>];                 // counts per wavefront and digit, 16 bits each; then the tile's keys and tokens in order
     __shared__ uint32_t base[1 << kSortBits], total[1 << kSortBits], wave_sum[2][kSortWaves];
     uint16_t *count = (uint16_t *)space;
     const int digits = 1 << a.bits, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, mine = threadIdx.x;
     const int64_t begin = (int64_t)blockIdx.x * a.piece, end = min(begin + a.piece, a.n);
-    uint32_t key[kSortRounds], token[kSortRounds];
+    uint32_t key[ROUNDS], token[ROUNDS];
     auto request = [&](int64_t tile) {
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r) {
-            const int64_t i = min(tile + (wave * kSortRounds + r) * kWave + lane, end - 1);
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int64_t i = min(tile + (wave * ROUNDS + r) * kWave + lane, end - 1);
             key[r] = sort_key<I, FIRST>(a, i);
             token[r] = FIRST ? (uint32_t)i : a.tokens[i];
         }
@@ -183,13 +191,13 @@ __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
     if (mine < digits) base[mine] = total[mine] = 0;
     __syncthreads();
     // total: tokens of every digit; base: those of earlier pieces
-    if (a.pieces <= kSortAlone) {
+    if (a.n <= kSortAlone) {
         count_digits<I, FIRST>(a, 0, begin, mine, kSortBlock, base);
         count_digits<I, FIRST>(a, begin, a.n, mine, kSortBlock, total);
         __syncthreads();
         if (mine < digits) total[mine] += base[mine];
     } else {
-        const int slices = kSortBlock >> a.bits, digit = mine & (digits - 1), groups = (a.pieces + kSortGroup - 1) / kSortGroup, own = (int)blockIdx.x / kSortGroup;
+        const int slices = kSortBlock >> a.bits, digit = mine & (digits - 1), groups = (a.pieces + kGroup - 1) / kGroup, own = (int)blockIdx.x / kGroup;
         uint32_t all = 0, before = mine < digits ? a.counts[(int64_t)blockIdx.x * digits + mine] : 0;
         for (int g0 = mine >> a.bits; g0 < groups; g0 += 32 * slices) {
             uint32_t v[32];
@@ -210,23 +218,23 @@ __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
         const uint32_t smaller = threads_before(mine < digits ? total[mine] : 0, wave_sum[0]);
         if (mine < digits) base[mine] += smaller;
     }
-    for (int64_t tile = begin; tile < end; tile += kSortTile) {
+    for (int64_t tile = begin; tile < end; tile += kTile) {
         if (tile > begin) request(tile);
         for (int c = mine; c < (kSortWaves << a.bits) / 2; c += kSortBlock) space[c] = 0;
         __syncthreads();
-        uint32_t place[kSortRounds];
-        uint64_t same[kSortRounds];                        // lanes of the same digit
+        uint32_t place[ROUNDS];
+        uint64_t same[ROUNDS];                        // lanes of the same digit
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r)
-            same[r] = equal_digits(key[r] >> a.shift & (digits - 1), a.bits, __ballot(tile + (wave * kSortRounds + r) * kWave + lane < end));
+        for (int r = 0; r < ROUNDS; ++r)
+            same[r] = equal_digits(key[r] >> a.shift & (digits - 1), a.bits, __ballot(tile + (wave * ROUNDS + r) * kWave + lane < end));
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r) {            // the first of them adds them all to the wavefront's count
+        for (int r = 0; r < ROUNDS; ++r) {            // the first of them adds them all to the wavefront's count
             const uint32_t at = (uint32_t)wave << a.bits | (key[r] >> a.shift & (digits - 1));
             place[r] = 0;
             if (same[r] && lane == __builtin_ctzll(same[r])) place[r] = atomicAdd(&space[at >> 1], (uint32_t)__popcll(same[r]) << (at & 1) * 16) >> (at & 1) * 16 & 0xffff;
         }
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r)
+        for (int r = 0; r < ROUNDS; ++r)
             place[r] = __shfl(place[r], same[r] ? __builtin_ctzll(same[r]) : lane) + __popcll(same[r] & ((1ull << lane) - 1));
         __syncthreads();
         uint32_t here = 0;                                 // the tile's tokens of digit `mine`
@@ -246,23 +254,23 @@ __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
         }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r) {
+        for (int r = 0; r < ROUNDS; ++r) {
             const uint32_t digit = key[r] >> a.shift & (digits - 1);
             place[r] += total[digit] + count[wave << a.bits | digit];
         }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kSortRounds; ++r)
-            if (tile + (wave * kSortRounds + r) * kWave + lane < end) {
+        for (int r = 0; r < ROUNDS; ++r)
+            if (tile + (wave * ROUNDS + r) * kWave + lane < end) {
                 space[place[r]] = key[r];
-                space[kSortTile + place[r]] = token[r];
+                space[kTile + place[r]] = token[r];
             }
         __syncthreads();
-        const int filled = (int)min((int64_t)kSortTile, end - tile);
+        const int filled = (int)min((int64_t)kTile, end - tile);
         for (int j = mine; j < filled; j += kSortBlock) {
             const uint32_t k = space[j], digit = k >> a.shift & (digits - 1), to = base[digit] + (uint32_t)j - total[digit];
             a.keys_out[to] = k;
-            a.tokens_out[to] = space[kSortTile + j];
+            a.tokens_out[to] = space[kTile + j];
         }
         __syncthreads();
         if (mine < digits) base[mine] += here;
@@ -651,13 +659,26 @@ struct GradPlan {
     int32_t each, groups;        // sums
     size_t lists, counts, where, part, bytes;      // offsets; four lists of n words begin at `lists`
 };
+template <int ROUNDS>
+static int launch_sort_pass(const SortArgs &sort, const GradPlan &p, bool first, hag_dtype_t id_type, hipStream_t s) {
+    typedef void (*kernel_t)(SortArgs);
+    const bool wide = id_type == HAG_I64;
+    const kernel_t count = !first ? (kernel_t)sort_count_kernel<int32_t, false, ROUNDS> : wide ? (kernel_t)sort_count_kernel<int64_t, true, ROUNDS> : (kernel_t)sort_count_kernel<int32_t, true, ROUNDS>;
+    const kernel_t place = !first ? (kernel_t)sort_place_kernel<int32_t, false, ROUNDS> : wide ? (kernel_t)sort_place_kernel<int64_t, true, ROUNDS> : (kernel_t)sort_place_kernel<int32_t, true, ROUNDS>;
+    if (sort.n > kSortAlone) hipLaunchKernelGGL(count, dim3((unsigned)((p.pieces + kSortGroup<ROUNDS> - 1) / kSortGroup<ROUNDS>)), dim3(kSortBlock), 0, s, sort);
+    HIP_TRY(hipGetLastError());
+    hipLaunchKernelGGL(place, dim3((unsigned)p.pieces), dim3(kSortBlock), 0, s, sort);
+    HIP_TRY(hipGetLastError());
+    return HAG_OK;
+}
 static GradPlan grad_plan(int64_t n, int64_t rows, int64_t d, int vec) {
     GradPlan p = {};
     int key_bits = 1;
     while ((rows >> key_bits) > 0) ++key_bits;
     p.passes = (key_bits + kSortBits - 1) / kSortBits;
     p.bits = (key_bits + p.passes - 1) / p.passes;
-    p.piece = std::max<int64_t>(1, (n + (int64_t)kSortPieces * kSortTile - 1) / ((int64_t)kSortPieces * kSortTile)) * kSortTile;
+    const int64_t tile = (int64_t)kSortBlock * sort_rounds(n), group = 8 / sort_rounds(n);
+    p.piece = std::max<int64_t>(1, (n + kSortPieces * tile - 1) / (kSortPieces * tile)) * tile;
     p.pieces = (int32_t)((n + p.piece - 1) / p.piece);
     const int64_t side = kBlock / embed_lanes(d, vec);
     p.each = kEachMost;
@@ -665,7 +686,7 @@ static GradPlan grad_plan(int64_t n, int64_t rows, int64_t d, int vec) {
     p.groups = (int32_t)((n + side * p.each - 1) / (side * p.each));
     auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += (bytes + 255) / 256 * 256; return at; };
     p.lists = take((size_t)n * 4 * 4);
-    p.counts = take((size_t)(p.pieces + (p.pieces + kSortGroup - 1) / kSortGroup) * 4 << p.bits);
+    p.counts = take((size_t)(p.pieces + (p.pieces + group - 1) / group) * 4 << p.bits);
     p.where = take((size_t)rows * 4);
     p.part = take((size_t)p.groups * 2 * d * 4);
     return p;
@@ -779,13 +800,7 @@ int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, co
         sort.tokens = sort.tokens_out;
         sort.keys_out = lists + (pass & 1) * 2 * n;
         sort.tokens_out = sort.keys_out + n;
-        typedef void (*kernel_t)(SortArgs);
-        const kernel_t count = pass > 0 ? (kernel_t)sort_count_kernel<int32_t, false> : id_type == HAG_I64 ? (kernel_t)sort_count_kernel<int64_t, true> : (kernel_t)sort_count_kernel<int32_t, true>;
-        const kernel_t place = pass > 0 ? (kernel_t)sort_place_kernel<int32_t, false> : id_type == HAG_I64 ? (kernel_t)sort_place_kernel<int64_t, true> : (kernel_t)sort_place_kernel<int32_t, true>;
-        if (p.pieces > kSortAlone) hipLaunchKernelGGL(count, dim3((unsigned)((p.pieces + kSortGroup - 1) / kSortGroup)), dim3(kSortBlock), 0, s, sort);
-        HIP_TRY(hipGetLastError());
-        hipLaunchKernelGGL(place, dim3((unsigned)p.pieces), dim3(kSortBlock), 0, s, sort);
-        HIP_TRY(hipGetLastError());
+        if (const int rc = sort_rounds(n) == 1 ? launch_sort_pass<1>(sort, p, pass == 0, id_type, s) : launch_sort_pass<2>(sort, p, pass == 0, id_type, s)) return rc;
     }
     a.keys = sort.keys_out;
     a.tokens = sort.tokens_out;
