@@ -35,7 +35,7 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
     for (int t = 0; t < R; ++t) id[t] = ids[min(row0 + t * (kWave / LPR), a.n - 1)];
 #pragma unroll
     for (int t = 0; t < R; ++t) {
-        other[t] = id[t] == a.padding ? 0.f : NAN;
+        other[t] = id[t] == a.padding && a.padding != HAG_NO_PADDING ? 0.f : NAN;   // (HAG_NO_PADDING is a number that an id can be)
         if (id[t] < 0 || id[t] >= a.rows || id[t] == a.padding) id[t] = -1;
     }
     for (int col = l * V; col < a.d; col += LPR * V) {

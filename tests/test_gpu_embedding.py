@@ -209,3 +209,22 @@ def test_refusals(B):
         with pytest.raises(B.HagError) as err:
             call()
         assert err.value.code == B.HAG_EINVAL
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [3, 4, 16, 70, 300])
+def test_ids_of_the_lowest_number(B, d, dtype):
+    low = torch.iinfo(torch.int64).min                     # what a NaN is as an int64 on many hosts, and the number that stands for no padding
+    table = torch.randn(6, d, device="cuda").to(dtype)
+    ids = torch.tensor([low, 2, low, -1, low + 1], device="cuda")
+    none, some = B.embedding(table, ids), B.embedding(table, ids, padding=-1)
+    assert torch.equal(none[1], table[2]) and bool(torch.isnan(none[[0, 2, 3, 4]]).all())
+    assert torch.equal(some[1], table[2]) and bool(torch.isnan(some[[0, 2, 4]]).all()) and not bool(some[3].any())
+    assert not bool(B.embedding(table, ids, padding=low + 1)[4].any())
+    short = torch.tensor([torch.iinfo(torch.int32).min, 2], device="cuda", dtype=torch.int32)
+    assert bool(torch.isnan(B.embedding(table, short)[0]).all()) and not bool(B.embedding(table, short, padding=int(short[0]))[0].any())
+    for n in (5, 3000, 9000, 140000):
+        many = ids.repeat(n // 5)
+        gy = torch.ones(many.numel(), d, device="cuda", dtype=dtype)
+        got = B.embedding_grad(gy, many, 6, dtype=torch.float32)
+        assert bool((got[2] == n // 5).all()) and int(got.count_nonzero()) == d
