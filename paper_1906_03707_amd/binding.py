@@ -525,14 +525,22 @@ def _ids(ids, device):
     return HAG_I64 if ids.dtype == torch.int64 else HAG_I32
 
 
+def _padding(padding):
+    """As a 64-bit number; one that no id can be is no padding (ctypes would pass its low 64 bits)."""
+    padding = int(padding)
+    if padding == HAG_NO_PADDING:
+        raise ValueError("a padding of -2**63 cannot be told from none")
+    return padding if HAG_NO_PADDING < padding < 1 << 63 else HAG_NO_PADDING
+
+
 def embedding(table, ids, scale=1.0, padding=None):
-    """scale * table[ids] [*ids.shape, d] of a table [rows, d] (hag_embedding).  Ids equal to `padding` (any number, a row or not) give rows of zeros, ids that are
-    no row of the table rows of NaN."""
+    """scale * table[ids] [*ids.shape, d] of a table [rows, d] (hag_embedding).  Ids equal to `padding` (any number but -2**63, a row or not) give rows of zeros, ids that
+    are no row of the table rows of NaN."""
     device = _device()
     code, stride = _rows("table", table, device)
     id_code, (rows, d) = _ids(ids, device), table.shape
     y = table.new_empty((*ids.shape, d))
-    rc = lib().hag_embedding(ids.numel(), rows, d, code, table.data_ptr(), stride, id_code, ids.data_ptr(), HAG_NO_PADDING if padding is None else int(padding), scale,
+    rc = lib().hag_embedding(ids.numel(), rows, d, code, table.data_ptr(), stride, id_code, ids.data_ptr(), HAG_NO_PADDING if padding is None else _padding(padding), scale,
                              y.data_ptr(), _raw_stream())
     if rc != 0:
         _check(rc)
@@ -554,7 +562,7 @@ def embedding_grad(g_y, ids, rows, scale=1.0, padding=None, dtype=None):
     out = g_y.new_empty((rows, d), dtype=dtype)
     L = lib()
     ws = g_y.new_empty(_elements_of(L.hag_embedding_grad_workspace_bytes(n, rows, d), code))
-    rc = L.hag_embedding_grad(n, rows, d, code, g_y.data_ptr(), stride, id_code, ids.data_ptr(), HAG_NO_PADDING if padding is None else int(padding), scale,
+    rc = L.hag_embedding_grad(n, rows, d, code, g_y.data_ptr(), stride, id_code, ids.data_ptr(), HAG_NO_PADDING if padding is None else _padding(padding), scale,
                               code if dtype is None else _elements[dtype], out.data_ptr(), ws.data_ptr(), _raw_stream())
     if rc != 0:
         _check(rc)

@@ -228,3 +228,16 @@ def test_ids_of_the_lowest_number(B, d, dtype):
         gy = torch.ones(many.numel(), d, device="cuda", dtype=dtype)
         got = B.embedding_grad(gy, many, 6, dtype=torch.float32)
         assert bool((got[2] == n // 5).all()) and int(got.count_nonzero()) == d
+
+
+def test_padding_that_no_id_can_be(B):
+    table, gy = torch.randn(6, 8, device="cuda"), torch.randn(2, 8, device="cuda")
+    ids = torch.tensor([3, 2 ** 63 - 1], device="cuda")
+    for padding in (2 ** 64 + 3, 3 - 2 ** 64, -2 ** 63 - 1, 2 ** 63):              # their low 64 bits are one of the ids, or no padding
+        got = B.embedding(table, ids, padding=padding)
+        assert torch.equal(got[0], table[3]) and bool(torch.isnan(got[1]).all())
+        assert torch.equal(B.embedding_grad(gy, ids, 6, padding=padding)[3], gy[0])
+    assert not bool(B.embedding(table, ids, padding=2 ** 63 - 1)[1].any())
+    for call in (lambda: B.embedding(table, ids, padding=-2 ** 63), lambda: B.embedding_grad(gy, ids, 6, padding=-2 ** 63)):
+        with pytest.raises(ValueError):
+            call()
