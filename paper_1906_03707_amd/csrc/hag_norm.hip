@@ -2,8 +2,10 @@
 //   m = mean of x over a row, r = 1 / sqrt(mean of (x - m)^2 + eps), xh = (x - m) r, y = xh w + b
 //   u = g_y w:  g_x = r (u - mean(u) - xh mean(u xh)),  g_w = sum over rows of g_y xh,  g_b = sum over rows of g_y
 // A row is read once and stays in registers: LPR adjacent lanes hold K vectors of 16 bytes each (lane l vectors l, l + LPR, ...), sums over a row are moves
-// between those lanes.  Statistics in fp32: the mean of the differences from the row's first element (rows of one value, however large, then have that
-// mean and no deviation), the variance of the deviations from the mean.  Rows of more than 1024 columns take a workgroup, of more than 8192 are read again for every sum.
+// between those lanes.  Statistics in fp32: a first mean m of the differences from the row's first element (rows of one value, however large, then have that
+// mean and no deviation), then the sums of the deviations from it and of their squares.  The mean of the deviations is what m is off by: rounded to the grid of its own size (half of
+// the spread for a row of 1e8 and 1e8 + 8), or by as much as the first element's grid where that stands out.  It is taken out of the mean, of the variance and of the deviations.
+// Rows of more than 1024 columns take a workgroup, of more than 8192 are read again for every sum.
 #include "hag_elem.hpp"
 
 namespace hag {
@@ -67,6 +69,12 @@ __device__ __forceinline__ float inverse_root(float v) {
     return r > 0.f && r < INFINITY ? better : r;           // (v infinite, zero or no number: as it is)
 }
 
+// mean of the squares of (deviations - off), off their mean; NaN stays
+__device__ __forceinline__ float variance(float squares, float off) {
+    const float v = fmaf(-off, off, squares);
+    return v < 0.f ? 0.f : v;
+}
+
 // Threads of a workgroup whose rows have LPR lanes (backward: twice as many where rows have a wavefront or less, so that there are half as many partial sums), and the rows
 // that a wavefront (or the workgroup) takes side by side.
 template <int LPR>
@@ -86,7 +94,7 @@ __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
     const int l = threadIdx.x % LPR;
     const int64_t row0 = ((int64_t)blockIdx.x * (kNormBlock<LPR> / kTaker) + threadIdx.x / kTaker) * (kSide<LPR> * R) + threadIdx.x % kTaker / LPR;
     const T *x = (const T *)a.x;
-    float v[R][K][V], first[R], m[R], r[R];
+    float v[R][K][V], first[R], m[R], off[R], r[R];
     int turn = 0;
     {
         Raw raw[R][K];
@@ -116,19 +124,24 @@ __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
             s += col < a.d ? part : 0.f;
         }
         m[t] = first[t] + row_sums<LPR>(make_float2(s, 0.f), lds, turn).x * a.inv_d;
-        s = 0.f;
+        float2 q = make_float2(0.f, 0.f);                  // squares of the deviations, deviations
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int col = (l + LPR * k) * V;
-            float part = 0.f;
+            float2 part = make_float2(0.f, 0.f);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 v[t][k][e] -= m[t];
-                part += !TAIL || col + e < a.d ? v[t][k][e] * v[t][k][e] : 0.f;
+                part.x += !TAIL || col + e < a.d ? v[t][k][e] * v[t][k][e] : 0.f;
+                part.y += !TAIL || col + e < a.d ? v[t][k][e] : 0.f;
             }
-            s += col < a.d ? part : 0.f;
+            q.x += col < a.d ? part.x : 0.f;
+            q.y += col < a.d ? part.y : 0.f;
         }
-        r[t] = inverse_root(row_sums<LPR>(make_float2(s, 0.f), lds, turn).x * a.inv_d + a.eps);
+        q = row_sums<LPR>(q, lds, turn);
+        off[t] = q.y * a.inv_d;
+        m[t] += off[t];
+        r[t] = inverse_root(variance(q.x * a.inv_d, off[t]) + a.eps);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -142,7 +155,7 @@ __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
             const int64_t row = row0 + t * kSide<LPR>;
             if (row >= a.n) continue;
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[t][k][e] = v[t][k][e] * r[t] * w[e] + b[e];
+            for (int e = 0; e < V; ++e) v[t][k][e] = (v[t][k][e] - off[t]) * r[t] * w[e] + b[e];
             store_vec((T *)a.out + row * a.d + col, TAIL ? a.d - col : V, v[t][k]);
         }
     }
@@ -323,14 +336,18 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *__restri
 
 // Rows that registers do not hold: a workgroup of 1024 reads its row again for every sum.
 constexpr int kWide = 1024;
-__device__ __forceinline__ float wide_sum(float v, float *lds) {
-    v = lanes_sum<kWave>(v);
+__device__ __forceinline__ float2 wide_sums(float2 v, float2 *lds) {
+    v.x = lanes_sum<kWave>(v.x);
+    v.y = lanes_sum<kWave>(v.y);
     __syncthreads();
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
     __syncthreads();
-    v = 0.f;
+    v = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < kWide / kWave; ++w) v += lds[w];
+    for (int w = 0; w < kWide / kWave; ++w) {
+        v.x += lds[w].x;
+        v.y += lds[w].y;
+    }
     return v;
 }
 
@@ -340,40 +357,45 @@ __device__ __forceinline__ float param(const void *p, int param32, T, int c) { r
 
 template <typename T>
 __global__ __launch_bounds__(kWide) void norm_wide_kernel(NormArgs a) {
-    __shared__ float lds[kWide / kWave];
+    __shared__ float2 lds[kWide / kWave];
     const int64_t row = blockIdx.x;
     const T *p = (const T *)a.x + row * a.x_stride;
     const float first = (float)p[0];
-    float s = 0.f;
-    for (int c = threadIdx.x; c < a.d; c += kWide) s += (float)p[c] - first;
-    const float m = first + wide_sum(s, lds) * a.inv_d;
-    s = 0.f;
-    for (int c = threadIdx.x; c < a.d; c += kWide) { const float v = (float)p[c] - m; s += v * v; }
-    const float r = inverse_root(wide_sum(s, lds) * a.inv_d + a.eps);
+    float2 s = make_float2(0.f, 0.f);
+    for (int c = threadIdx.x; c < a.d; c += kWide) s.x += (float)p[c] - first;
+    const float m = first + wide_sums(s, lds).x * a.inv_d;
+    s.x = 0.f;
     for (int c = threadIdx.x; c < a.d; c += kWide) {
-        const float xh = ((float)p[c] - m) * r;
+        const float v = (float)p[c] - m;
+        s.x += v * v;
+        s.y += v;
+    }
+    s = wide_sums(s, lds);
+    const float off = s.y * a.inv_d, r = inverse_root(variance(s.x * a.inv_d, off) + a.eps);
+    for (int c = threadIdx.x; c < a.d; c += kWide) {
+        const float xh = ((float)p[c] - m - off) * r;
         ((T *)a.out)[row * a.d + c] = (T)(xh * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f) + (a.bias ? param(a.bias, a.param32, T(), c) : 0.f));
     }
     if (threadIdx.x == 0) {
-        if (a.mean) a.mean[row] = m;
+        if (a.mean) a.mean[row] = m + off;
         if (a.rstd) a.rstd[row] = r;
     }
 }
 
 template <typename T>
 __global__ __launch_bounds__(kWide) void norm_grad_wide_kernel(NormArgs a) {
-    __shared__ float lds[kWide / kWave];
+    __shared__ float2 lds[kWide / kWave];
     const int64_t row = blockIdx.x;
     const T *p = (const T *)a.x + row * a.x_stride, *g = (const T *)a.gy + row * a.gy_stride;
     const float m = a.mean_in[row], r = a.rstd_in[row];
-    float s1 = 0.f, s2 = 0.f;
+    float2 s = make_float2(0.f, 0.f);
     for (int c = threadIdx.x; c < a.d; c += kWide) {
         const float u = (float)g[c] * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f);
-        s1 += u;
-        s2 += u * (((float)p[c] - m) * r);
+        s.x += u;
+        s.y += u * (((float)p[c] - m) * r);
     }
-    s1 = wide_sum(s1, lds) * a.inv_d;
-    s2 = wide_sum(s2, lds) * a.inv_d;
+    s = wide_sums(s, lds);
+    const float s1 = s.x * a.inv_d, s2 = s.y * a.inv_d;
     for (int c = threadIdx.x; c < a.d; c += kWide) {
         const float u = (float)g[c] * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f);
         ((T *)a.out)[row * a.d + c] = (T)(r * (u - s1 - ((float)p[c] - m) * r * s2));

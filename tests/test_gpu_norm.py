@@ -225,3 +225,35 @@ def test_refusals(B):
         with pytest.raises(B.HagError) as err:
             call()
         assert err.value.code == B.HAG_EINVAL
+
+
+@pytest.mark.parametrize("d", [2, 16, 100, 251, 512, 1000, 1500, 4096, 8192, 16500])
+def test_rows_that_are_not_around_their_first_element(B, d):
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    # a sum's path to a lane's result, through the lanes and through the wavefronts has no more than 40 additions (of more than 8192 columns: and one for each 1024)
+    depth = 40 + (d // 1024 if d > 8192 else 0)
+    for dtype, large in ((torch.float32, 1e4), (torch.float32, -3e6), (torch.bfloat16, 1e4), (torch.float16, 6e4)):
+        x = torch.randn(40, d, device="cuda", generator=gen).to(dtype)
+        x[:30, 0] = large
+        x[10:20, 1:] -= 50
+        x64 = x.double()
+        m = x64.mean(1)
+        size = (x64 - m[:, None]).abs().mean(1)
+        mean = B.layer_norm(x)[1].double()
+        # the deviations' roundings, their sum's, the mean's own
+        assert bool(((mean - m).abs() <= (depth + 3) * EPS * size + 2 * EPS * m.abs()).all())
+
+
+@pytest.mark.parametrize("d", [2, 8, 64, 250, 1000, 4098, 9000])
+def test_rows_whose_mean_is_no_fp32_number(B, d):
+    for low, step in ((1e8, 8.0), (-1e8, 8.0), (2.0 ** 64, 2.0 ** 41), (2.0 ** 24, 2.0)):   # two neighbours in fp32
+        x = torch.full((3, d), low, device="cuda")
+        x[:, 1::2] += step
+        x[2] = x[2].flip(0)
+        y, mean, rstd = B.layer_norm(x, eps=0.0)
+        want = torch.ones(3, d, device="cuda", dtype=torch.float64)
+        want[:2, ::2] = -1
+        want[2, 1::2] = -1
+        # sums of steps and of their squares, exact; 1 / d, its products with them, the variance, its reciprocal root (half of them), the deviations and their product
+        assert bool(((y.double() - want).abs() <= 12 * EPS).all()) and bool(((rstd.double() * step / 2 - 1).abs() <= 8 * EPS).all())
+        assert bool(((mean.double() - (x.double()[:, 0] + x.double()[:, 1]) / 2).abs() <= step / 2).all())
