@@ -412,7 +412,7 @@ int hag_softmax_loss_grad(int64_t n, int64_t classes, const float *z, const int6
  * type of g_y or HAG_F32.  Ids that are `padding` or no row send no gradient.  Fixed order of additions: the same bits every time.
  *
  * hag_layer_norm: y = (x - mean) * rstd * weight + bias per row of x [n, d]; mean [n], rstd [n] = 1 / sqrt(variance + eps) (either may be NULL: not kept), weight and
- * bias [d] of the type of x or HAG_F32 (either may be NULL: 1 and 0).
+ * bias [d] of the type of x or HAG_F32 (either may be NULL: 1 and 0).  Finite rows of any size; rstd is an fp32 number (a spread below 1e-19 takes an eps).
  * hag_layer_norm_grad: the gradients at x, weight and bias (the latter two of param_dtype; either may be NULL: not wanted) of a loss whose gradient
  * at y is g_y, with mean and rstd as the forward call left them.  Fixed order of additions.
  *

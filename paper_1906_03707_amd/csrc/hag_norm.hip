@@ -69,11 +69,24 @@ __device__ __forceinline__ float inverse_root(float v) {
     return r > 0.f && r < INFINITY ? better : r;           // (v infinite, zero or no number: as it is)
 }
 
+// Rows of finite numbers whose differences or squares add up beyond fp32 are taken again times 2^-80: below 2^48 then, squares of differences of 2^20 columns add up to less
+// than 2^118.  Some deviation was 2^54 or more, so what is lost below 2^-149 is nothing beside the spread.  (fp16 numbers cannot get there.)
+constexpr float kFarScale = 0x1p-80f;
+template <typename T>
+constexpr bool kFarRows = !std::is_same<T, f16_t>::value;
+
 // mean of the squares of (deviations - off), off their mean; NaN stays
 __device__ __forceinline__ float variance(float squares, float off) {
     const float v = fmaf(-off, off, squares);
     return v < 0.f ? 0.f : v;
 }
+
+// (x - m) r by halves: the difference of two fp32 numbers may be no fp32 number, that of their halves is one
+__device__ __forceinline__ float normed(float x, float m, float r) { return fmaf(x, 0.5f, -0.5f * m) * (2.f * r); }
+
+__device__ __forceinline__ float param(const void *p, int param32, float, int c) { return ((const float *)p)[c]; }
+template <typename T>
+__device__ __forceinline__ float param(const void *p, int param32, T, int c) { return param32 ? ((const float *)p)[c] : (float)((const T *)p)[c]; }
 
 // Threads of a workgroup whose rows have LPR lanes (backward: twice as many where rows have a wavefront or less, so that there are half as many partial sums), and the rows
 // that a wavefront (or the workgroup) takes side by side.
@@ -83,6 +96,38 @@ template <int LPR>
 constexpr int kGradBlock = LPR <= kWave ? 2 * kBlock : LPR;
 template <int LPR>
 constexpr int kSide = LPR <= kWave ? kWave / LPR : 1;
+
+// A row beyond fp32 (`here`; other rows' lanes go along), read again for every sum: rows that nothing but a broken training meets, so what counts is that the ordinary ones do not
+// hold registers for them.
+template <typename T, int LPR>
+__device__ __forceinline__ void norm_far_row(const NormArgs &a, int64_t row, bool here, float2 (*lds)[16], int &turn) {
+    const int l = threadIdx.x % LPR;
+    const T *p = (const T *)a.x + min(row, a.n - 1) * a.x_stride;
+    const float first = (float)p[0] * kFarScale;
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll 1
+    for (int c = l; c < a.d; c += LPR) s.x += (float)p[c] * kFarScale - first;
+    const float m = first + row_sums<LPR>(s, lds, turn).x * a.inv_d;
+    s.x = 0.f;
+#pragma unroll 1
+    for (int c = l; c < a.d; c += LPR) {
+        const float v = (float)p[c] * kFarScale - m;
+        s.x += v * v;
+        s.y += v;
+    }
+    s = row_sums<LPR>(s, lds, turn);
+    const float off = s.y * a.inv_d, r = inverse_root(variance(s.x * a.inv_d, off) + a.eps * kFarScale * kFarScale);
+    if (!here) return;
+#pragma unroll 1
+    for (int c = l; c < a.d; c += LPR) {
+        const float xh = ((float)p[c] * kFarScale - m - off) * r;
+        ((T *)a.out)[row * a.d + c] = (T)(xh * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f) + (a.bias ? param(a.bias, a.param32, T(), c) : 0.f));
+    }
+    if (l == 0) {
+        if (a.mean) a.mean[row] = (m + off) / kFarScale;
+        if (a.rstd) a.rstd[row] = r * kFarScale;
+    }
+}
 
 // Bound by reading x and writing y.  Every lane requests R rows one after the other before it needs the first.  232965 x 128 fp32 40 us, bf16 21 (5.9 and 5.8 TB/s; a copy: 5.3),
 // 56944 x 251 bf16, rows at any address, 15.7 (3.6).
@@ -95,6 +140,7 @@ __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
     const int64_t row0 = ((int64_t)blockIdx.x * (kNormBlock<LPR> / kTaker) + threadIdx.x / kTaker) * (kSide<LPR> * R) + threadIdx.x % kTaker / LPR;
     const T *x = (const T *)a.x;
     float v[R][K][V], first[R], m[R], off[R], r[R];
+    uint32_t far = 0;                                      // bits of rows beyond fp32
     int turn = 0;
     {
         Raw raw[R][K];
@@ -142,6 +188,7 @@ __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
         off[t] = q.y * a.inv_d;
         m[t] += off[t];
         r[t] = inverse_root(variance(q.x * a.inv_d, off[t]) + a.eps);
+        if (kFarRows<T> && !(q.x < INFINITY) && row0 + t * kSide<LPR> < a.n) far |= 1u << t;
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -153,7 +200,7 @@ __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
 #pragma unroll
         for (int t = 0; t < R; ++t) {
             const int64_t row = row0 + t * kSide<LPR>;
-            if (row >= a.n) continue;
+            if (row >= a.n || far >> t & 1) continue;
 #pragma unroll
             for (int e = 0; e < V; ++e) v[t][k][e] = (v[t][k][e] - off[t]) * r[t] * w[e] + b[e];
             store_vec((T *)a.out + row * a.d + col, TAIL ? a.d - col : V, v[t][k]);
@@ -162,10 +209,14 @@ __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
 #pragma unroll
     for (int t = 0; t < R; ++t) {
         const int64_t row = row0 + t * kSide<LPR>;
-        if (l == 0 && row < a.n) {
+        if (l == 0 && row < a.n && !(far >> t & 1)) {
             if (a.mean) a.mean[row] = m[t];
             if (a.rstd) a.rstd[row] = r[t];
         }
+    }
+    if (kFarRows<T> && __any(far != 0)) {                  // (a row of more than a wavefront: the same in all of them)
+#pragma unroll 1
+        for (int t = 0; t < R; ++t) norm_far_row<T, LPR>(a, row0 + t * kSide<LPR>, far >> t & 1, lds, turn);
     }
 }
 
@@ -221,7 +272,7 @@ __global__ __launch_bounds__(kGradBlock<LPR>) void norm_grad_kernel(NormArgs a) 
                 for (int e = 0; e < V; ++e) {
                     const bool in = here && (!TAIL || col + e < a.d);
                     const float g = in ? (float)q.g[t][k][e] : 0.f;
-                    xh[k][e] = in ? ((float)q.x[t][k][e] - q.m[t]) * q.r[t] : 0.f;
+                    xh[k][e] = in ? normed((float)q.x[t][k][e], q.m[t], q.r[t]) : 0.f;
                     u[k][e] = g * w[k][e];
                     gw[k][e] += g * xh[k][e];              // (columns beyond the row's end: not read)
                     gb[k][e] += g;
@@ -351,34 +402,36 @@ __device__ __forceinline__ float2 wide_sums(float2 v, float2 *lds) {
     return v;
 }
 
-__device__ __forceinline__ float param(const void *p, int param32, float, int c) { return ((const float *)p)[c]; }
-template <typename T>
-__device__ __forceinline__ float param(const void *p, int param32, T, int c) { return param32 ? ((const float *)p)[c] : (float)((const T *)p)[c]; }
-
 template <typename T>
 __global__ __launch_bounds__(kWide) void norm_wide_kernel(NormArgs a) {
     __shared__ float2 lds[kWide / kWave];
     const int64_t row = blockIdx.x;
     const T *p = (const T *)a.x + row * a.x_stride;
-    const float first = (float)p[0];
-    float2 s = make_float2(0.f, 0.f);
-    for (int c = threadIdx.x; c < a.d; c += kWide) s.x += (float)p[c] - first;
-    const float m = first + wide_sums(s, lds).x * a.inv_d;
-    s.x = 0.f;
-    for (int c = threadIdx.x; c < a.d; c += kWide) {
-        const float v = (float)p[c] - m;
-        s.x += v * v;
-        s.y += v;
+    float scale = 1.f, m, off, r;
+    for (;;) {                                             // (once, for rows beyond fp32 twice)
+        const float first = (float)p[0] * scale;
+        float2 s = make_float2(0.f, 0.f);
+        for (int c = threadIdx.x; c < a.d; c += kWide) s.x += (float)p[c] * scale - first;
+        m = first + wide_sums(s, lds).x * a.inv_d;
+        s.x = 0.f;
+        for (int c = threadIdx.x; c < a.d; c += kWide) {
+            const float v = (float)p[c] * scale - m;
+            s.x += v * v;
+            s.y += v;
+        }
+        s = wide_sums(s, lds);
+        off = s.y * a.inv_d;
+        r = inverse_root(variance(s.x * a.inv_d, off) + a.eps * scale * scale);
+        if (!kFarRows<T> || scale != 1.f || s.x < INFINITY) break;
+        scale = kFarScale;
     }
-    s = wide_sums(s, lds);
-    const float off = s.y * a.inv_d, r = inverse_root(variance(s.x * a.inv_d, off) + a.eps);
     for (int c = threadIdx.x; c < a.d; c += kWide) {
-        const float xh = ((float)p[c] - m - off) * r;
+        const float xh = ((float)p[c] * scale - m - off) * r;
         ((T *)a.out)[row * a.d + c] = (T)(xh * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f) + (a.bias ? param(a.bias, a.param32, T(), c) : 0.f));
     }
     if (threadIdx.x == 0) {
-        if (a.mean) a.mean[row] = m + off;
-        if (a.rstd) a.rstd[row] = r;
+        if (a.mean) a.mean[row] = (m + off) / scale;
+        if (a.rstd) a.rstd[row] = r * scale;
     }
 }
 
@@ -392,13 +445,13 @@ __global__ __launch_bounds__(kWide) void norm_grad_wide_kernel(NormArgs a) {
     for (int c = threadIdx.x; c < a.d; c += kWide) {
         const float u = (float)g[c] * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f);
         s.x += u;
-        s.y += u * (((float)p[c] - m) * r);
+        s.y += u * normed((float)p[c], m, r);
     }
     s = wide_sums(s, lds);
     const float s1 = s.x * a.inv_d, s2 = s.y * a.inv_d;
     for (int c = threadIdx.x; c < a.d; c += kWide) {
         const float u = (float)g[c] * (a.weight ? param(a.weight, a.param32, T(), c) : 1.f);
-        ((T *)a.out)[row * a.d + c] = (T)(r * (u - s1 - ((float)p[c] - m) * r * s2));
+        ((T *)a.out)[row * a.d + c] = (T)(r * (u - s1 - normed((float)p[c], m, r) * s2));
     }
 }
 
@@ -411,7 +464,7 @@ __global__ __launch_bounds__(kBlock) void norm_wide_sums_kernel(NormArgs a) {
     if (c < a.d) {
         for (int64_t row = (int64_t)blockIdx.y * (kBlock / kWave) + wave; row < a.n; row += (int64_t)gridDim.y * (kBlock / kWave)) {
             const float g = (float)((const T *)a.gy)[row * a.gy_stride + c];
-            gw += g * (((float)((const T *)a.x)[row * a.x_stride + c] - a.mean_in[row]) * a.rstd_in[row]);
+            gw += g * normed((float)((const T *)a.x)[row * a.x_stride + c], a.mean_in[row], a.rstd_in[row]);
             gb += g;
         }
     }

@@ -257,3 +257,38 @@ def test_rows_whose_mean_is_no_fp32_number(B, d):
         # sums of steps and of their squares, exact; 1 / d, its products with them, the variance, its reciprocal root (half of them), the deviations and their product
         assert bool(((y.double() - want).abs() <= 12 * EPS).all()) and bool(((rstd.double() * step / 2 - 1).abs() <= 8 * EPS).all())
         assert bool(((mean.double() - (x.double()[:, 0] + x.double()[:, 1]) / 2).abs() <= step / 2).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [2, 7, 16, 64, 130, 512, 777, 1024, 1500, 4100, 8192, 9001])
+def test_rows_whose_squares_are_no_fp32_numbers(B, d, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    z = torch.randn(12, d, device="cuda", generator=gen)
+    near = torch.cat([z[:3], 3 * z[3:6] + 1])              # ordinary rows beside them, which must not change
+    x = torch.cat([near, 1e19 * z[:2], 1e25 * z[2:4], 1e30 + 1e29 * z[4:6], 6e37 * z[6:8].clamp(-5, 5), 3e38 * z[8:10].sign(), 1e36 * z[10:12].sign()]).to(dtype)
+    x = torch.cat([x, torch.tensor([[float("inf")], [float("nan")], [3.3e38]], device="cuda").to(dtype).expand(3, d)])
+    x[-3, 1:], x[-2, 0] = 1, 1
+    w, b = params(d, torch.float32, gen)
+    y, mean, rstd = B.layer_norm(x, w, b)
+    assert all(torch.equal(p[:6], q) for p, q in zip((y, mean, rstd), B.layer_norm(x[:6], w, b)))
+    assert bool(torch.isnan(y[-3:-1]).all()) and torch.equal(y[-1], b.to(dtype))
+    x, y, mean, rstd = x[:-3], y[:-3], mean[:-3], rstd[:-3]
+    x64 = x.double()
+    want, m, r, xh = forward64(x, w, b, 1e-5)
+    depth = 40 + (d // 1024 if d > 8192 else 0)            # additions on the way of a term into a row's sum
+    size = (x64 - m).abs().mean(1, keepdim=True)
+    dm = (depth + 3) * EPS * size + 2 * EPS * m.abs()
+    assert bool(((mean.double()[:, None] - m).abs() <= dm).all())
+    dr = (depth / 2 + 8) * EPS * r                         # squares and their sum, by half; the root; below 2^-126 the grid of small numbers
+    assert bool(((rstd.double()[:, None] - r).abs() <= dr + 2.0 ** -150).all())
+    # the deviations' mean is taken out of them, so their error is that of its sum
+    dxh = r * (depth + 4) * EPS * (size + (x64 - m).abs()) + xh.abs() * dr / r
+    dy = dxh * w.double().abs() + 3 * EPS * (xh.abs() * w.double().abs() + b.double().abs())
+    assert bool(((y.double() - want).abs() <= dy + HALF[dtype] * (want.abs() + dy)).all())
+    gy = torch.randn(x.shape, device="cuda", generator=gen).to(dtype)
+    gx, gw, gb = B.layer_norm_grad(gy, x, mean, rstd, w)
+    assert bool(torch.isfinite(gx).all()) and bool(torch.isfinite(gw).all())
+    check_grad((gx[:8], None, None), gy[:8], x[:8], mean[:8], rstd[:8], w)
+    xh = (x64 - mean.double()[:, None]) * rstd.double()[:, None]
+    terms = gy.double() * xh
+    assert bool(((gw.double() - terms.sum(0)).abs() <= (len(x) + 4) * EPS * terms.abs().sum(0)).all())
