@@ -418,8 +418,8 @@ int hag_softmax_loss_grad(int64_t n, int64_t classes, const float *z, const int6
  *
  * hag_clip_gradients: *norm (fp32, device) = the 2-norm of all elements of all tensors as one vector, and out = in * (max_norm / norm where the norm is above
  * max_norm, else 1) for each of them.  `list` is host memory, read during the call; out may be in (then nothing is written where nothing is clipped), else they must not overlap.
- * Squares are added up in fp64 in a fixed order.  An infinite norm makes finite elements 0 and infinite ones NaN, a NaN makes all NaN; max_norm may be
- * infinite.  Captured calls keep the addresses they were captured with. */
+ * Squares are added up in fp64 in a fixed order.  An infinite element makes finite ones 0 and infinite ones NaN, a NaN makes all NaN (a norm of finite
+ * elements that is above fp32's range is infinite in *norm only); max_norm may be infinite.  Captured calls keep the addresses they were captured with. */
 #define HAG_NO_PADDING INT64_MIN
 int hag_embedding(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, const void *table, int64_t table_stride, hag_dtype_t id_type, const void *ids,
                   int64_t padding, float scale, void *y, void *stream);

@@ -113,6 +113,13 @@ __device__ __forceinline__ void scale_unit(const T *p, T *out, int64_t count, fl
     }
 }
 
+// The same with a factor that is no fp32 number: rare, so without vectors in flight, whose registers the ordinary way would have to hold too (44 -> 71, bf16 32.3 -> 33.4 us).
+template <typename T>
+__device__ __forceinline__ void scale_unit_far(const T *p, T *out, int64_t count, double c) {
+#pragma unroll 1
+    for (int64_t i = threadIdx.x; i < count; i += kBlock) out[i] = (T)(float)((double)(float)p[i] * c);
+}
+
 // Bound by reading once more and writing: 30 M fp32 elements into other tensors 38 us (6.3 TB/s: part of what is read is still in the caches).  Every workgroup adds up all partial
 // sums itself, in one order, rather than wait for one more launch.  What is left above one read and one write is the second read; tensors of this size would fit the
 // registers and LDS of all compute units, but a wait of all workgroups for each other hangs where another stream holds some of their places.
@@ -127,15 +134,25 @@ __global__ __launch_bounds__(kBlock) void clip_scale_kernel(ClipArgs a, const do
         for (int u = 0; u < 8; ++u) s += i + u * kBlock < a.partials ? v[u] : 0.;
     }
     const double total = sqrt(block_sum64(s, lds));
-    const float c = total <= max_norm ? 1.f : (float)(max_norm / total);   // (a NaN: NaN; an infinite norm: 0, and NaN for the infinite elements)
+    const double factor = total <= max_norm ? 1. : max_norm / total;       // (a NaN: NaN; an infinite norm: 0, and NaN for the infinite elements)
+    const float c = (float)factor;
     if (blockIdx.x == 0 && a.partial_at == 0 && threadIdx.x == 0) *norm = (float)total;
     if ((int)blockIdx.x >= a.units) return;                // no element at all: the launch is there for the norm
     const int t = clip_tensor(a, blockIdx.x);
     if (c == 1.f && a.t[t].out == a.t[t].in) return;
     const int64_t begin = (int64_t)(blockIdx.x - a.t[t].first_unit) * a.unit, count = min(a.unit, a.t[t].count - begin);
-    if (a.t[t].dtype == HAG_F32) scale_unit((const float *)a.t[t].in + begin, (float *)a.t[t].out + begin, count, c);
-    else if (a.t[t].dtype == HAG_BF16) scale_unit((const bf16_t *)a.t[t].in + begin, (bf16_t *)a.t[t].out + begin, count, c);
-    else scale_unit((const f16_t *)a.t[t].in + begin, (f16_t *)a.t[t].out + begin, count, c);
+    // A factor below 2^-126 has fewer bits in fp32, or none, where its products with gradients as large as their norm are ordinary numbers: those are taken in 64 bits.
+    const bool far = c < 0x1p-126f;
+    auto scale = [&](auto e) {
+        using T = decltype(e);
+        const T *in = (const T *)a.t[t].in + begin;
+        T *out = (T *)a.t[t].out + begin;
+        if (far) scale_unit_far(in, out, count, factor);
+        else scale_unit(in, out, count, c);
+    };
+    if (a.t[t].dtype == HAG_F32) scale(float());
+    else if (a.t[t].dtype == HAG_BF16) scale(bf16_t());
+    else scale(f16_t());
 }
 
 }  // namespace hag

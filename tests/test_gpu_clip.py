@@ -138,3 +138,23 @@ def test_refusals(B):
             B.clip_gradients([t], bad)
         assert err.value.code == B.HAG_EINVAL
     assert bool((t == 1).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("count", [5, 3000, 4096, 70001])
+def test_factors_below_fp32(B, count, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    z = torch.rand(count, device="cuda", generator=gen) + 0.25
+    for large, max_norm in ((3e38, 1.0), (3e38, 1e-3), (3e38, 1e-12), (1e37, 1e-3), (2e38, 1e-30)):
+        t = (large * (z - 0.5).clamp(-1, 1)).to(dtype)
+        assert norm64([t]) / max_norm > 2.0 ** 126
+        into = [torch.empty_like(t)]
+        norm = B.clip_gradients([t], max_norm, out=into)
+        want = t.double() * (max_norm / norm64([t]))
+        assert bool(((into[0].double() - want).abs() <= (3 * EPS + HALF[dtype]) * want.abs() * (1 + 1e-3) + TINY[dtype]).all())     # as any other factor
+        again = [t.clone()]
+        assert torch.equal(B.clip_gradients(again, max_norm), norm) and torch.equal(again[0], into[0])
+    for bad in (float("inf"), float("nan")):
+        t[1] = bad
+        norm = B.clip_gradients([t], 1.0, out=into).item()
+        assert (math.isnan(norm) and bool(torch.isnan(into[0]).all())) if math.isnan(bad) else (norm == math.inf and math.isnan(into[0][1].item()) and int(into[0].count_nonzero()) == 1)
