@@ -21,6 +21,17 @@ static inline int id_switch(hag_dtype_t t, F f) {
     return t == HAG_I64 ? f(int64_t()) : f(int32_t());
 }
 
+// A launch has fewer than 2^32 threads in x: f(first, count) launches workgroups first .. first + count of the `blocks` that the sizes call for.
+template <typename F>
+static inline int launch_parts(int64_t blocks, int64_t threads, F f) {
+    const int64_t most = ((int64_t)1 << 31) / threads;
+    for (int64_t first = 0; first < blocks; first += most) {
+        f(first, std::min(most, blocks - first));
+        HIP_TRY(hipGetLastError());
+    }
+    return HAG_OK;
+}
+
 // 16 bytes of a row: memory operations of that width at any address that suits one element, which gfx950's global loads and stores take.
 template <typename T>
 constexpr int kVec = 16 / (int)sizeof(T);

@@ -329,6 +329,7 @@ struct GradArgs {
     int64_t n, rows;
     int32_t d, each;                 // entries of a group of lanes
     int32_t groups;                  // workgroups of the sums
+    int32_t first;                   // workgroup that this launch begins with
     float scale;
 };
 
@@ -423,7 +424,7 @@ __global__ __launch_bounds__(kBlock) void embed_sum_kernel(GradArgs a) {
     __shared__ uint8_t flags[G];
     uint32_t *keys = key_store + 1;
     const int l = threadIdx.x % LPR, col = ((int)blockIdx.y * LPR + l) * V;
-    const int64_t begin = (int64_t)blockIdx.x * G * a.each;
+    const int64_t block = a.first + (int64_t)blockIdx.x, begin = block * G * a.each;
     const int count = (int)min((int64_t)G * a.each, a.n - begin);
     for (int i = threadIdx.x; i < count; i += 2 * kBlock) {
         const int64_t at = begin + i, then = begin + min(i + kBlock, count - 1);
@@ -453,7 +454,7 @@ __global__ __launch_bounds__(kBlock) void embed_sum_kernel(GradArgs a) {
         },
         [&](bool first, float (&s)[V]) {
             if (col >= a.d) return;
-            store_cols(a.part + ((int64_t)blockIdx.x * 2 + (first ? 0 : 1)) * a.d + col, TAIL ? a.d - col : V, s);
+            store_cols(a.part + (block * 2 + (first ? 0 : 1)) * a.d + col, TAIL ? a.d - col : V, s);
         });
 }
 
@@ -465,11 +466,12 @@ __global__ __launch_bounds__(kBlock) void embed_join_kernel(GradArgs a) {
     constexpr int V = kVec<T>, G = kBlock / LPR;
     __shared__ float lds[G][LPR * V];
     const int l = threadIdx.x % LPR, g = threadIdx.x / LPR;
-    if ((int)blockIdx.x < a.groups - 1) {
-        const int64_t per = (int64_t)G * a.each, begin = (int64_t)blockIdx.x * per, next = begin + per;
+    const int64_t block = a.first + (int64_t)blockIdx.x;
+    if (block < a.groups - 1) {
+        const int64_t per = (int64_t)G * a.each, begin = block * per, next = begin + per;
         const uint32_t run = a.keys[next - 1], first = a.keys[begin], before = begin > 0 ? a.keys[begin - 1] : kNone, after = a.keys[next];
         // the last workgroup that it reaches: those whose first entry is of this run, 256 looked at a time (the first of them with the loads above)
-        int64_t lo = blockIdx.x;
+        int64_t lo = block;
         uint32_t probe = a.keys[min(lo + 1 + threadIdx.x, (int64_t)a.groups - 1) * per];
         if (run == (uint32_t)a.rows || after != run || (first == run && before == run)) return;          // padding; done; began earlier
         for (;;) {
@@ -483,12 +485,12 @@ __global__ __launch_bounds__(kBlock) void embed_join_kernel(GradArgs a) {
 #pragma unroll
         for (int e = 0; e < V; ++e) s[e] = 0.f;
         if (col < a.d) {
-            for (int64_t b0 = (int64_t)blockIdx.x + g; b0 <= lo; b0 += 4 * G) {
+            for (int64_t b0 = block + g; b0 <= lo; b0 += 4 * G) {
                 float p[4][V];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const int64_t b = min(b0 + u * G, lo);
-                    const float *q = a.part + (b * 2 + (b == blockIdx.x ? 1 : 0)) * a.d;
+                    const float *q = a.part + (b * 2 + (b == block ? 1 : 0)) * a.d;
 #pragma unroll
                     for (int e = 0; e < V; ++e) p[u][e] = q[TAIL ? min(col + e, a.d - 1) : col + e];
                 }
@@ -502,7 +504,7 @@ __global__ __launch_bounds__(kBlock) void embed_join_kernel(GradArgs a) {
         for (int e = 0; e < V; ++e) lds[g][l * V + e] = s[e];
         __syncthreads();
         if (g > 0 || col >= a.d) return;
-        for (int h = 1; h < G && (int64_t)blockIdx.x + h <= lo; ++h)
+        for (int h = 1; h < G && block + h <= lo; ++h)
 #pragma unroll
             for (int e = 0; e < V; ++e) s[e] += lds[h][l * V + e];
 #pragma unroll
@@ -512,7 +514,7 @@ __global__ __launch_bounds__(kBlock) void embed_join_kernel(GradArgs a) {
     }
     if (blockIdx.y > 0) return;
     const int lane = threadIdx.x % kWave;
-    const int64_t row0 = ((int64_t)((int)blockIdx.x - max(a.groups - 1, 0)) * (kBlock / kWave) + threadIdx.x / kWave) * kWave, row = row0 + lane;
+    const int64_t row0 = ((block - max(a.groups - 1, 0)) * (kBlock / kWave) + threadIdx.x / kWave) * kWave, row = row0 + lane;
     bool empty = row < a.rows;
     if (empty && a.n > 0) {
         const uint32_t at = a.where[row];
@@ -550,7 +552,7 @@ __global__ __launch_bounds__(kBlock) void embed_few_kernel(GradArgs a, const I *
     __shared__ uint8_t flags[G];
     uint32_t *keys = key_store + 1;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, l = threadIdx.x % LPR, g = threadIdx.x / LPR;
-    const int64_t row0 = (int64_t)blockIdx.x * kFewRows;
+    const int64_t row0 = (a.first + (int64_t)blockIdx.x) * kFewRows;
     for (int c = threadIdx.x; c < kWaves * kFewRows; c += kBlock) count[c / kFewRows][c % kFewRows] = 0;
     __syncthreads();
     uint32_t row[kFewRounds], rank[kFewRounds];
@@ -721,9 +723,13 @@ int hag_embedding(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, const v
             return lanes_switch(embed_lanes(d, kVec<T>), d % kVec<T> != 0, [&](auto lanes, auto tail) {
                 constexpr int LPR = decltype(lanes)::value;
                 constexpr int64_t kRows = kBlock / LPR * kEmbedRows;
-                hipLaunchKernelGGL((embed_kernel<T, I, LPR, decltype(tail)::value>), dim3((unsigned)((n + kRows - 1) / kRows)), dim3(kBlock), 0, (hipStream_t)stream, a);
-                HIP_TRY(hipGetLastError());
-                return (int)HAG_OK;
+                return launch_parts((n + kRows - 1) / kRows, kBlock, [&](int64_t first, int64_t count) {
+                    EmbedArgs part = a;
+                    part.ids = (const I *)ids + first * kRows;
+                    part.y = (T *)y + first * kRows * d;
+                    part.n = std::min(count * kRows, n - first * kRows);
+                    hipLaunchKernelGGL((embed_kernel<T, I, LPR, decltype(tail)::value>), dim3((unsigned)count), dim3(kBlock), 0, (hipStream_t)stream, part);
+                });
             });
         });
     });
@@ -767,10 +773,11 @@ int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, co
         return pick([&](auto e, auto o, auto lanes, auto tails) {
             return id_switch(id_type, [&](auto k) {
                 using I = decltype(k);
-                hipLaunchKernelGGL((embed_few_kernel<decltype(e), decltype(o), I, decltype(lanes)::value, decltype(tails)::value>), dim3((unsigned)((rows + kFewRows - 1) / kFewRows)),
-                                   dim3(kBlock), 0, s, a, (const I *)ids, padding);
-                HIP_TRY(hipGetLastError());
-                return (int)HAG_OK;
+                return launch_parts((rows + kFewRows - 1) / kFewRows, kBlock, [&](int64_t first, int64_t count) {
+                    a.first = (int32_t)first;
+                    hipLaunchKernelGGL((embed_few_kernel<decltype(e), decltype(o), I, decltype(lanes)::value, decltype(tails)::value>), dim3((unsigned)count), dim3(kBlock), 0, s, a,
+                                       (const I *)ids, padding);
+                });
             });
         });
     const GradPlan p = grad_plan(n, rows, d, vec);
@@ -808,17 +815,21 @@ int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, co
     a.part = (float *)(ws + p.part);
     a.each = p.each;
     a.groups = p.groups;
-    const unsigned joins = (unsigned)(p.groups - 1) + (unsigned)((rows + kBlock - 1) / kBlock);
+    const int64_t joins = p.groups - 1 + (rows + kBlock - 1) / kBlock;
     return pick([&](auto e, auto o, auto lanes, auto tails) {
         using T = decltype(e);
         using O = decltype(o);
         constexpr int LPR = decltype(lanes)::value;
         constexpr bool TAIL = decltype(tails)::value;
-        hipLaunchKernelGGL((embed_sum_kernel<T, O, LPR, TAIL>), dim3((unsigned)p.groups, chunks), dim3(kBlock), 0, s, a);
-        HIP_TRY(hipGetLastError());
-        hipLaunchKernelGGL((embed_join_kernel<T, O, LPR, TAIL>), dim3(joins, chunks), dim3(kBlock), 0, s, a);
-        HIP_TRY(hipGetLastError());
-        return (int)HAG_OK;
+        const int rc = launch_parts(p.groups, kBlock, [&](int64_t first, int64_t count) {
+            a.first = (int32_t)first;
+            hipLaunchKernelGGL((embed_sum_kernel<T, O, LPR, TAIL>), dim3((unsigned)count, chunks), dim3(kBlock), 0, s, a);
+        });
+        if (rc != HAG_OK) return rc;
+        return launch_parts(joins, kBlock, [&](int64_t first, int64_t count) {
+            a.first = (int32_t)first;
+            hipLaunchKernelGGL((embed_join_kernel<T, O, LPR, TAIL>), dim3((unsigned)count, chunks), dim3(kBlock), 0, s, a);
+        });
     });
 }
 

@@ -489,6 +489,25 @@ static NormShape norm_shape(int64_t d, int vec) {
 }
 
 typedef void (*norm_kernel_t)(NormArgs);
+// Workgroups that take `rows` rows each, whatever a launch holds.
+template <typename T>
+static int launch_rows(norm_kernel_t kernel, const NormArgs &a, int64_t rows, int threads, hipStream_t s) {
+    return launch_parts((a.n + rows - 1) / rows, threads, [&](int64_t first, int64_t count) {
+        const int64_t at = first * rows;
+        NormArgs part = a;
+        part.n = std::min(count * rows, a.n - at);
+        part.x = (const T *)a.x + at * a.x_stride;
+        part.x_extent = (part.n - 1) * a.x_stride + a.d;
+        part.gy = a.gy ? (const T *)a.gy + at * a.gy_stride : nullptr;
+        part.gy_extent = (part.n - 1) * a.gy_stride + a.d;
+        part.out = (T *)a.out + at * a.d;
+        part.mean_in = a.mean_in ? a.mean_in + at : nullptr;
+        part.rstd_in = a.rstd_in ? a.rstd_in + at : nullptr;
+        part.mean = a.mean ? a.mean + at : nullptr;
+        part.rstd = a.rstd ? a.rstd + at : nullptr;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3((unsigned)threads), 0, s, part);
+    });
+}
 template <typename T, template <int, int> class F>
 static norm_kernel_t norm_pick(NormShape s) {
     switch (s.lpr) {
@@ -577,15 +596,9 @@ int hag_layer_norm(int64_t n, int64_t d, hag_dtype_t dtype, const void *x, int64
     return elem_switch(dtype, [&](auto e) {
         using T = decltype(e);
         const NormShape s = norm_shape(d, kVec<T>);
-        if (s.k == 0) {
-            hipLaunchKernelGGL(norm_wide_kernel<T>, dim3((unsigned)n), dim3(kWide), 0, (hipStream_t)stream, a);
-        } else {
-            const int64_t rows = norm_side(s, false) * norm_rows(s.lpr, s.k, kVec<T>);
-            const norm_kernel_t kernel = d % kVec<T> ? norm_pick<T, Forward<T, true>::template Of>(s) : norm_pick<T, Forward<T, false>::template Of>(s);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)((n + rows - 1) / rows)), dim3((unsigned)norm_block(s, false)), 0, (hipStream_t)stream, a);
-        }
-        HIP_TRY(hipGetLastError());
-        return (int)HAG_OK;
+        if (s.k == 0) return launch_rows<T>(norm_wide_kernel<T>, a, 1, kWide, (hipStream_t)stream);
+        const norm_kernel_t kernel = d % kVec<T> ? norm_pick<T, Forward<T, true>::template Of>(s) : norm_pick<T, Forward<T, false>::template Of>(s);
+        return launch_rows<T>(kernel, a, norm_side(s, false) * norm_rows(s.lpr, s.k, kVec<T>), norm_block(s, false), (hipStream_t)stream);
     });
 }
 
@@ -630,8 +643,7 @@ int hag_layer_norm_grad(int64_t n, int64_t d, hag_dtype_t dtype, const void *g_y
             a.g_b = g_bias;
         }
         if (shape.k == 0) {
-            if (n > 0) hipLaunchKernelGGL(norm_grad_wide_kernel<T>, dim3((unsigned)n), dim3(kWide), 0, s, a);
-            HIP_TRY(hipGetLastError());
+            if (const int rc = launch_rows<T>(norm_grad_wide_kernel<T>, a, 1, kWide, s)) return rc;
             if (params) hipLaunchKernelGGL(norm_wide_sums_kernel<T>, dim3((unsigned)((d + kWave - 1) / kWave), (unsigned)groups), dim3(kBlock), 0, s, a);
         } else {
             const size_t lds = shape.lpr <= kWave ? (size_t)(norm_block(shape, true) / kWave) * shape.lpr * shape.k * kVec<T> * 2 * sizeof(float) : 0;
