@@ -541,9 +541,15 @@ __global__ __launch_bounds__(kBlock) void embed_join_kernel(GradArgs a) {
 
 // ------------------------------------------------------------------------------------------------------------------ few tokens
 
-// Up to kFew tokens: one launch, 9 us for 777 tokens of 37 columns in 4096 rows where the path above takes 25.  (2048 tokens: 11 and 26, but 33 and 29 if all name one row; 4096: 11 and
-// 27, 67 and 33.)  A workgroup looks through all ids for those of its 32 rows, sorts them by row in LDS and adds up their runs, which are whole.
+// Few tokens: one launch.  A workgroup looks through all ids for those of its 32 rows, sorts them by row in LDS and adds up their runs, which are whole.
+// Bound by the busiest workgroup: 9 us (a launch and the host) and 1 us for each 8000 to 10000 elements that its rows get (4000 where d is no multiple of a vector), whatever the other
+// compute units do; the path above takes 14 to 16 us, 20 to 35 where many wide rows are empty.  Fewer rows than tokens are categories, of which some are in demand: few tokens of those are what one workgroup
+// can take in that time.  As many rows as tokens are names, most of them given once: a workgroup gets few tokens, unless nearly all of them name one row.  fp32, us by this path / that, for ids
+// spread evenly and for all of one row:
+//   2000 x 64 of 16 rows 19 / 16, 19 / 16    2000 x 128 of 300 10 / 16, 32 / 16     2000 x 1024 of 16 247 / 14, 251 / 17    2000 x 1024 of 300 42 / 16, 249 / 34
+//   1000 x 37 of 4096 9.3 / 16, 16 / 17      1000 x 250 of 4096 9.5 / 20, 50 / 21   250 x 1024 of 4096 12 / 33, 40 / 32     2000 x 1024 of 4096 16 / 35, 252 / 35 (a tenth of them one row: 32 / 35)
 constexpr int kFew = 2048, kFewRows = 32, kFewRounds = kFew / kBlock;
+static bool few_tokens(int64_t n, int64_t rows, int64_t d) { return n <= kFew && (rows >= n || n * d <= 1 << 17); }
 template <typename T, typename O, typename I, int LPR, bool TAIL>
 __global__ __launch_bounds__(kBlock) void embed_few_kernel(GradArgs a, const I *ids, int64_t padding) {
     constexpr int V = kVec<T>, G = kBlock / LPR, kWaves = kBlock / kWave;
@@ -737,7 +743,7 @@ int hag_embedding(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, const v
 
 size_t hag_embedding_grad_workspace_bytes(int64_t n, int64_t rows, int64_t d) {
     if (embed_refusal(n, rows, d, HAG_I64, 0)) return 0;
-    return n <= kFew ? 16 : std::max(grad_plan(n, rows, d, 4).bytes, grad_plan(n, rows, d, 8).bytes);
+    return few_tokens(n, rows, d) ? 16 : std::max(grad_plan(n, rows, d, 4).bytes, grad_plan(n, rows, d, 8).bytes);
 }
 
 int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, const void *g_y, int64_t g_y_stride, hag_dtype_t id_type, const void *ids, int64_t padding,
@@ -769,7 +775,7 @@ int hag_embedding_grad(int64_t n, int64_t rows, int64_t d, hag_dtype_t dtype, co
             return lanes_switch(lpr, tail, [&](auto lanes, auto tails) { return out_dtype == dtype ? f(e, e, lanes, tails) : f(e, float(), lanes, tails); });
         });
     };
-    if (n <= kFew)
+    if (few_tokens(n, rows, d))
         return pick([&](auto e, auto o, auto lanes, auto tails) {
             return id_switch(id_type, [&](auto k) {
                 using I = decltype(k);

@@ -241,3 +241,18 @@ def test_padding_that_no_id_can_be(B):
     for call in (lambda: B.embedding(table, ids, padding=-2 ** 63), lambda: B.embedding_grad(gy, ids, 6, padding=-2 ** 63)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("kind", ["even", "skew", "one"])
+@pytest.mark.parametrize("n,rows,d", [(2000, 16, 1024), (2048, 33, 201), (2048, 33, 64), (2048, 33, 65), (700, 6000, 376), (700, 6000, 371), (64, 2, 2049), (65, 65, 5000), (5, 3, 40001), (2, 1, 70001),
+                                      (1, 3, 262144), (1, 3, 262145)])
+def test_gradient_of_few_wide_tokens(B, n, rows, d, kind):
+    gen = torch.Generator(device="cuda").manual_seed(n + rows + d)
+    ids = make_ids(n, rows, kind, gen)
+    ids[3::7] = -1
+    for dtype in TYPES:
+        gy = torch.randn(n, d, device="cuda", generator=gen).to(dtype)
+        got = B.embedding_grad(gy, ids, rows, 1.5, -1)
+        check_grad(got, gy, ids, rows, 1.5, -1)
+        assert torch.equal(got, B.embedding_grad(gy, ids.int(), rows, 1.5, -1))
+    assert not bool(B.embedding_grad(gy, torch.full_like(ids, -1), rows, padding=-1).any())

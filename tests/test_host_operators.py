@@ -72,3 +72,12 @@ def test_clip_refusals():
     for fields in ((P, P, -1, 0), (P, P, 5, 1), (P, P, 5, 4), (0, P, 5, 0), (P, 0, 5, 0), (P, P, 1 << 50, 0)):
         refused(L.hag_clip_gradients(1, entry(*fields), 1.0, P, P, None))
     assert L.hag_clip_workspace_bytes(-1) == 0 and L.hag_clip_workspace_bytes(3) > 0
+
+
+def test_wide_tokens_of_fewer_rows_are_shared():
+    """One workgroup takes the few tokens of 32 rows by itself; where that is much and there are fewer rows than tokens, these are put in order and shared, which takes a workspace."""
+    size = B.lib().hag_embedding_grad_workspace_bytes
+    for n, rows, d in ((2000, 16, 1024), (2000, 74, 1024), (2048, 16, 100), (300, 200, 1030), (2, 1, 1 << 20)):
+        assert size(n, rows, d) >= 16 * n + 4 * rows
+    for n, rows, d in ((777, 4096, 37), (74, 74, 64), (2000, 74, 64), (0, 5, 1 << 20), (2000, 2000, 1024)):
+        assert size(n, rows, d) == 16
