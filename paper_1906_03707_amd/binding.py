@@ -559,9 +559,11 @@ def embedding_grad(g_y, ids, rows, scale=1.0, padding=None, dtype=None):
         raise ValueError(f"unsupported dtype {dtype}")
     if rows < 0:
         raise ValueError("rows must not be negative")
-    out = g_y.new_empty((rows, d), dtype=dtype)
     L = lib()
-    ws = g_y.new_empty(_elements_of(L.hag_embedding_grad_workspace_bytes(n, rows, d), code))
+    nbytes = 0 if rows >> 31 else L.hag_embedding_grad_workspace_bytes(n, rows, d)
+    if not nbytes:                                         # sizes that are refused, before anything of that size is made
+        _check(L.hag_embedding_grad(n, min(rows, 1 << 31), d, code, None, stride, id_code, None, HAG_NO_PADDING, scale, code, None, None, None))
+    out, ws = g_y.new_empty((rows, d), dtype=dtype), g_y.new_empty(_elements_of(nbytes, code))
     rc = L.hag_embedding_grad(n, rows, d, code, g_y.data_ptr(), stride, id_code, ids.data_ptr(), HAG_NO_PADDING if padding is None else _padding(padding), scale,
                               code if dtype is None else _elements[dtype], out.data_ptr(), ws.data_ptr(), _raw_stream())
     if rc != 0:

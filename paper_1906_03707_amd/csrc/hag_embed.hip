@@ -709,7 +709,7 @@ extern "C" {
 // what both calls ask of their sizes
 static const char *embed_refusal(int64_t n, int64_t rows, int64_t d, hag_dtype_t id_type, int64_t stride) {
     if (n < 0 || rows < 0 || d <= 0) return "n < 0, rows < 0 or d <= 0";
-    if (n > 0x7fffffffLL || rows > 0x7fffffffLL - 1 || d > (1 << 20)) return "n and rows must be below 2^31, d at most 2^20";
+    if (n > 0x7fffffffLL || rows > 0x7fffffffLL || d > (1 << 20)) return "n and rows must be below 2^31, d at most 2^20";
     if (id_type != HAG_I32 && id_type != HAG_I64) return "ids are HAG_I32 or HAG_I64";
     if (stride < 0) return "negative row stride";
     return nullptr;

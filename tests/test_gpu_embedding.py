@@ -256,3 +256,19 @@ def test_gradient_of_few_wide_tokens(B, n, rows, d, kind):
         check_grad(got, gy, ids, rows, 1.5, -1)
         assert torch.equal(got, B.embedding_grad(gy, ids.int(), rows, 1.5, -1))
     assert not bool(B.embedding_grad(gy, torch.full_like(ids, -1), rows, padding=-1).any())
+
+
+def test_sizes_are_refused_before_anything_is_made(B):
+    gy, ids = torch.randn(2, 4, device="cuda"), torch.tensor([2 ** 31 - 3, 5], device="cuda")
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    for rows in (2 ** 31, 2 ** 40, 2 ** 64 + 5):
+        with pytest.raises(B.HagError) as err:
+            B.embedding_grad(gy, ids, rows)
+        assert err.value.code == B.HAG_EINVAL and torch.cuda.max_memory_allocated() == before
+    for call in (lambda: B.embedding_grad(gy[:, :0], ids, 9), lambda: B.embedding_grad(gy[:0, :0], ids[:0], 9)):
+        with pytest.raises(B.HagError) as err:
+            call()
+        assert err.value.code == B.HAG_EINVAL
+    assert B.embedding_grad(gy, ids, 0).shape == (0, 4)

@@ -98,3 +98,15 @@ def test_layer_norm_of_many_rows(B, n, d):
     u, xh = gy[:1].double() * w64, dev * r
     want = r * (u - u.mean(1, keepdim=True) - xh * (u * xh).mean(1, keepdim=True))
     assert bool(((gx[some].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -16) * want.abs() + 2.0 ** -14).all())
+
+
+def test_gradient_of_as_many_rows_as_there_may_be(B):
+    rows, n = 2 ** 31 - 1, 3000
+    need(40 * GB)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for many in (2, n):                                    # few tokens, and tokens put in order
+        ids = torch.randint(0, rows, (many,), device="cuda", generator=gen)
+        ids[0], ids[1] = rows - 1, rows                    # the last row, the first that is none
+        got = B.embedding_grad(torch.ones(many, 1, device="cuda", dtype=torch.bfloat16), ids, rows)
+        want, count = torch.unique(ids[ids < rows], return_counts=True)
+        assert torch.equal(got[want, 0], count.bfloat16()) and sum(int(p.count_nonzero()) for p in got.split(1 << 28)) == want.numel()

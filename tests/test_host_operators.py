@@ -81,3 +81,15 @@ def test_wide_tokens_of_fewer_rows_are_shared():
         assert size(n, rows, d) >= 16 * n + 4 * rows
     for n, rows, d in ((777, 4096, 37), (74, 74, 64), (2000, 74, 64), (0, 5, 1 << 20), (2000, 2000, 1024)):
         assert size(n, rows, d) == 16
+
+
+def test_sizes_at_their_limits():
+    """n and rows are below 2^31: the largest are not refused (nothing is launched: a NULL pointer comes after the sizes), the next are."""
+    L = B.lib()
+    for n, rows in ((2, BIG - 1), (BIG - 1, 2)):
+        refused(L.hag_embedding(n, rows, 4, 0, None, 4, 4, P, -1, 1.0, P, None))
+        assert L.hag_last_error() == b"NULL pointer"
+        refused(L.hag_embedding_grad(n, rows, 4, 0, None, 4, 4, P, -1, 1.0, 0, P, P, None))
+        assert L.hag_last_error() == b"NULL pointer"
+        assert L.hag_embedding_grad_workspace_bytes(n, rows, 4) > 0
+        assert L.hag_embedding_grad_workspace_bytes(n + (n > 2), rows + (rows > 2), 4) == 0
