@@ -1,6 +1,7 @@
 """Build libhag.so (host C++ + HIP kernels for gfx950) in-tree with hipcc."""
 from __future__ import annotations
 
+import glob
 import os
 import re
 import subprocess
@@ -16,8 +17,7 @@ SOURCES = [os.path.join(HERE, "csrc", f) for f in (
     # element type (and reduction) so that they compile side by side
     "hag_gather_f32_sum.hip", "hag_gather_f32_max.hip", "hag_gather_i32_sum.hip", "hag_gather_i32_max.hip",
     "hag_component_f32.hip", "hag_component_i32.hip", "hag_dense.hip")]
-HEADERS = [os.path.join(HERE, "csrc", f) for f in ("hag_internal.hpp", "hag_device_common.hpp", "hag_gather.inc",
-                                                   "hag_component.inc")] + [os.path.join(ROOT, "include", "hag.h")]
+HEADERS = sorted(glob.glob(os.path.join(HERE, "csrc", "*.hpp")) + glob.glob(os.path.join(HERE, "csrc", "*.inc"))) + [os.path.join(ROOT, "include", "hag.h")]
 
 
 def build_library(force: bool = True, verbose: bool = False) -> str:
