@@ -407,14 +407,15 @@ int hag_softmax_loss_grad(int64_t n, int64_t classes, const float *z, const int6
  * number of rows of a table are below 2^31, d is in 1 .. 2^20.  `workspace` is 16-byte aligned, of the bytes that the function above the call names.
  *
  * hag_embedding: y [n, d] = scale * table[ids], table [rows, d], ids [n] (HAG_I32 or HAG_I64).  An id equal to `padding` gives a row of zeros whatever the table
- * holds (HAG_NO_PADDING: there is none), any other id that is no row of the table a row of NaN.
+ * holds (HAG_NO_PADDING, which no padding can be: there is none), any other id that is no row of the table a row of NaN.
  * hag_embedding_grad: g_table [rows, d] = scale * the sum of the rows of g_y [n, d] whose id names the row, 0 for rows that none names; g_table has the
  * type of g_y or HAG_F32.  Ids that are `padding` or no row send no gradient.  Fixed order of additions: the same bits every time.
  *
  * hag_layer_norm: y = (x - mean) * rstd * weight + bias per row of x [n, d]; mean [n], rstd [n] = 1 / sqrt(variance + eps) (either may be NULL: not kept), weight and
  * bias [d] of the type of x or HAG_F32 (either may be NULL: 1 and 0).  Finite rows of any size; rstd is an fp32 number (a spread below 1e-19 takes an eps).
  * hag_layer_norm_grad: the gradients at x, weight and bias (the latter two of param_dtype; either may be NULL: not wanted) of a loss whose gradient
- * at y is g_y, with mean and rstd as the forward call left them.  Fixed order of additions.
+ * at y is g_y, with mean and rstd as the forward call left them (in fp32: a row whose spread is a few units in the last place of its mean loses it here).  Fixed order
+ * of additions.
  *
  * hag_clip_gradients: *norm (fp32, device) = the 2-norm of all elements of all tensors as one vector, and out = in * (max_norm / norm where the norm is above
  * max_norm, else 1) for each of them.  `list` is host memory, read during the call; out may be in (then nothing is written where nothing is clipped), else they must not overlap.

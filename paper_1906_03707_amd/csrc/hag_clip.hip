@@ -85,7 +85,8 @@ __global__ __launch_bounds__(kBlock) void clip_sums_kernel(ClipArgs a, double *_
     if (threadIdx.x == 0) partial[a.partial_at + blockIdx.x] = sum;
 }
 
-// Last piece first: the end of every unit was read last and is still in the caches, where streaming stores leave it (30 M fp32 elements into other tensors 74 -> 62 us).
+// Last piece first: the end of every unit was read last and is still in the caches, where streaming stores leave it (30 M fp32 elements into other tensors 72 -> 59 us;
+// with an update that reads them next 155 -> 148, but 4 M elements 26 -> 33: ordinary stores would leave those in the caches).
 template <typename T>
 __device__ __forceinline__ void scale_unit(const T *p, T *out, int64_t count, float c) {
     constexpr int V = kVec<T>;

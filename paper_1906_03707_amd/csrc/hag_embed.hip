@@ -19,8 +19,9 @@ struct EmbedArgs {
 };
 
 // Bound by writing y (and by reading the table where it exceeds the caches).  LPR lanes move a row, 16 bytes each, four rows at a time: the ids first, then the rows they name.
-// Streaming stores leave the caches to the table (524288 rows of 232965, 128 columns: fp32 91 -> 85 us, bf16 43 -> 41).  370000 rows of 74, 64 fp32 columns: 16.3 us, 5.8 TB/s written
-// (a fill: 6.4); a call on 74 rows 7.5 us, which is the host's.
+// Streaming stores leave the caches to the table: 524288 rows of 232965, 128 columns, ids spread evenly / some rows in demand: fp32 88 -> 83 us, 84 -> 53, bf16 40.7 -> 37.8, 29.9 -> 27.8.  What
+// reads y next finds less of it there: with a layer norm after it fp32 186 -> 181, but bf16 84 -> 90, and 56944 rows of as many, fp32, 21.8 -> 23.9, 370000 x 64 of 74 47 -> 52.
+// 370000 rows of 74, 64 fp32 columns: 16.4 us, 5.8 TB/s written (a fill: 6.4); a call on 74 rows 7.5 us, which is the host's.
 constexpr int kEmbedRows = 4;
 template <typename T, typename I, int LPR, bool TAIL>
 __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {

@@ -129,8 +129,8 @@ __device__ __forceinline__ void norm_far_row(const NormArgs &a, int64_t row, boo
     }
 }
 
-// Bound by reading x and writing y.  Every lane requests R rows one after the other before it needs the first.  232965 x 128 fp32 40 us, bf16 21 (5.9 and 5.8 TB/s; a copy: 5.3),
-// 56944 x 251 bf16, rows at any address, 15.7 (3.6).
+// Bound by reading x and writing y.  Every lane requests R rows one after the other before it needs the first.  232965 x 128 fp32 40.5 us, bf16 21.2 (5.9 and 5.7 TB/s; a copy: 5.3).
+// 56944 x 251 bf16 15.2 us, x 256 12.1: the same bytes from and to memory, but 1.4 times the vector instructions (which columns count) and twice the stores (rows' ends, element by element).
 template <typename T, int LPR, int K, int R, bool TAIL>
 __global__ __launch_bounds__(kNormBlock<LPR>) void norm_kernel(NormArgs a) {
     __shared__ float2 lds[2][16];
@@ -533,7 +533,8 @@ static norm_kernel_t norm_pick(NormShape s) {
         return F<1024, 1>::kernel;
     }
 }
-// Rows one after the other that a lane requests at once.  Forward: 16 columns' worth (232965 x 128: fp32 40.3 us with 4 rows, 40.5 with 2; bf16 21.3 and 20.7).
+// Rows one after the other that a lane requests at once.  Forward: 16 columns' worth, against 8: 65536 x 512 fp32 43.5 us and 45.4, 232965 x 128 bf16 21.3 and 22.0, 56944 x 251 bf16 15.3
+// and 17.3, but 232965 x 128 fp32 40.4 and 39.7, 370000 x 64 fp32 34.0 and 33.2.
 constexpr int norm_rows(int lpr, int k, int vec) { return lpr > kWave || k * vec >= 16 ? 1 : 16 / (k * vec); }
 constexpr int norm_grad_rows(int lpr, int k) { return lpr <= kWave && k == 1 ? 2 : 1; }
 // Threads of a workgroup, and the rows that it takes side by side.

@@ -145,7 +145,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
 
 def clip_gradients(parameters, max_norm):
     """Scales the gradients of `parameters` (those that have one) down, in place, so that their 2-norm, taken as one vector, is at most max_norm.  The norm they had, a float32
-    scalar on the device: nothing waits for it.  An infinite norm leaves zeros and NaN, a NaN all NaN, so look at it before the parameters are changed where that can happen."""
+    scalar on the device: nothing waits for it.  An infinite gradient leaves zeros and NaN, a NaN all NaN, so look at it before the parameters are changed where that can happen."""
     grads = [p.grad for p in parameters if p.grad is not None]
     norm = binding.clip_gradients(grads, max_norm)
     if grads:
