@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
 // A token's key is its id, `rows` where it names no row: those come last and are left out.  Radix sort, low digits first, with stable passes of up to 10 bits:
 // counts per piece of the list, then every piece finds where each of its digits begins (the counts of smaller digits and of earlier pieces) and writes its tokens there.
 // Few bytes, so what it costs is the way of a piece through the steps of a pass: many loads at a time, few pieces to look back at.  524288 tokens, 9 bits: counts 5 us, places 12; a
-// gradient with pieces of 2048 tokens 122 us, of 4096 (half of the compute units idle) 123, of 1024 (twice as many to look back at) 137.
+// gradient with pieces of 2048 tokens 121 us, of 4096 (half of the compute units idle) 123, of 1024 (twice as many to look back at) 137.
 // Up to kSortShort tokens the tiles are half as long: twice as many compute units have one (12000 tokens of 64 columns 30.5 -> 28.6 us, 30000 34.9 -> 33.5; 370000 36 -> 43).
 constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / kWave, kSortBits = 10, kSortPieces = 256;
 constexpr int64_t kSortShort = 128 * kSortBlock, kSortAlone = 16 * kSortBlock;     // (so few tokens every piece counts itself)
@@ -279,7 +279,8 @@ __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(SortArgs a) {
 }
 
 // Up to kRankMost tokens are put in order by one launch instead of two passes: a token's place is the number of tokens that come before it, counted by comparing it with all of them (2 vector
-// instructions for 64 pairs, and LDS for the keys: a gradient of 8192 tokens 21 us where two passes make it 25, of 16384 38 and 27).  A workgroup places 32 tokens, 16 lanes each, out of all keys in LDS.
+// instructions for 64 pairs, and LDS for the keys: a gradient of 8192 tokens of 30000 rows 19.7 us where two passes make it 23.3, of 16384 38 and 27; of 300 rows, which take one pass, 4096
+// tokens 15.3 both ways, 8192 18.5 and 15.5).  A workgroup places 32 tokens, 16 lanes each, out of all keys in LDS.
 constexpr int kRankMost = 8192, kRankTokens = 32, kRankBlock = 512, kRankStreams = kRankBlock / kRankTokens, kRankAsk = kRankMost / kRankBlock;
 template <typename I>
 __global__ __launch_bounds__(kRankBlock) void sort_rank_kernel(SortArgs a) {
