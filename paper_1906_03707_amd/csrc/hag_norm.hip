@@ -6,7 +6,7 @@
 // mean and no deviation), then the sums of the deviations from it and of their squares.  The mean of the deviations is what m is off by: rounded to the grid of its own size (half of
 // the spread for a row of 1e8 and 1e8 + 8), or by as much as the first element's grid where that stands out.  It is taken out of the mean, of the variance and of the deviations.
 // Rows of more than 1024 columns take a workgroup, of more than 8192 are read again for every sum.
-#include "hag_elem.hpp"
+#include "hag_norm_common.hpp"
 
 namespace hag {
 
@@ -24,56 +24,9 @@ struct NormArgs {
     void *g_w, *g_b;                 // for one workgroup
 };
 
-// weight or bias of the columns of a vector; `otherwise` where there is none
-template <typename T, bool TAIL>
-__device__ __forceinline__ void load_params(const void *p, int param32, int col, int d, float otherwise, float (&v)[kVec<T>]) {
-#pragma unroll
-    for (int e = 0; e < kVec<T>; ++e) v[e] = otherwise;
-    if (!p || col >= d) return;
-    if (!param32) {
-        const typename VecOf<T>::type raw = load_vec((const T *)p + col, !TAIL || col + kVec<T> <= d, d - col);
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e) v[e] = (float)raw[e];
-        return;
-    }
-#pragma unroll
-    for (int q = 0; q < kVec<T>; q += 4) {
-        const typename VecOf<float>::type raw = load_vec((const float *)p + col + q, !TAIL || col + q + 4 <= d, d - col - q);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[q + e] = raw[e];
-    }
-}
-
-// Sums over a row, in all of its lanes.  Rows of up to 64 lanes: moves between lanes; longer ones: the workgroup, through LDS (two halves, used in turn, so that one barrier
-// a sum is enough).
-template <int LPR>
-__device__ __forceinline__ float2 row_sums(float2 v, float2 (*lds)[16], int &turn) {
-    v.x = lanes_sum<(LPR <= kWave ? LPR : kWave)>(v.x);
-    v.y = lanes_sum<(LPR <= kWave ? LPR : kWave)>(v.y);
-    if (LPR <= kWave) return v;
-    if (threadIdx.x % kWave == 0) lds[turn][threadIdx.x / kWave] = v;
-    __syncthreads();
-    v = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < LPR / kWave; ++w) {
-        v.x += lds[turn][w].x;
-        v.y += lds[turn][w].y;
-    }
-    turn ^= 1;
-    return v;
-}
-
-// 1 / sqrt(v): the hardware's (one unit in the last place), and one step of Newton's method (half of one)
-__device__ __forceinline__ float inverse_root(float v) {
-    const float r = rsqrtf(v), better = fmaf(0.5f * r, fmaf(-(v * r), r, 1.f), r);
-    return r > 0.f && r < INFINITY ? better : r;           // (v infinite, zero or no number: as it is)
-}
-
 // Rows of finite numbers whose differences or squares add up beyond fp32 are taken again times 2^-80: below 2^48 then, squares of differences of 2^20 columns add up to less
-// than 2^118.  Some deviation was 2^54 or more, so what is lost below 2^-149 is nothing beside the spread.  (fp16 numbers cannot get there.)
+// than 2^118.  Some deviation was 2^54 or more, so what is lost below 2^-149 is nothing beside the spread.  (fp16 numbers cannot get there: kFarRows.)
 constexpr float kFarScale = 0x1p-80f;
-template <typename T>
-constexpr bool kFarRows = !std::is_same<T, f16_t>::value;
 
 // mean of the squares of (deviations - off), off their mean; NaN stays
 __device__ __forceinline__ float variance(float squares, float off) {
@@ -83,19 +36,6 @@ __device__ __forceinline__ float variance(float squares, float off) {
 
 // (x - m) r by halves: the difference of two fp32 numbers may be no fp32 number, that of their halves is one
 __device__ __forceinline__ float normed(float x, float m, float r) { return fmaf(x, 0.5f, -0.5f * m) * (2.f * r); }
-
-__device__ __forceinline__ float param(const void *p, int param32, float, int c) { return ((const float *)p)[c]; }
-template <typename T>
-__device__ __forceinline__ float param(const void *p, int param32, T, int c) { return param32 ? ((const float *)p)[c] : (float)((const T *)p)[c]; }
-
-// Threads of a workgroup whose rows have LPR lanes (backward: twice as many where rows have a wavefront or less, so that there are half as many partial sums), and the rows
-// that a wavefront (or the workgroup) takes side by side.
-template <int LPR>
-constexpr int kNormBlock = LPR <= kWave ? kBlock : LPR;
-template <int LPR>
-constexpr int kGradBlock = LPR <= kWave ? 2 * kBlock : LPR;
-template <int LPR>
-constexpr int kSide = LPR <= kWave ? kWave / LPR : 1;
 
 // A row beyond fp32 (`here`; other rows' lanes go along), read again for every sum: rows that nothing but a broken training meets, so what counts is that the ordinary ones do not
 // hold registers for them.
@@ -385,23 +325,6 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *__restri
     }
 }
 
-// Rows that registers do not hold: a workgroup of 1024 reads its row again for every sum.
-constexpr int kWide = 1024;
-__device__ __forceinline__ float2 wide_sums(float2 v, float2 *lds) {
-    v.x = lanes_sum<kWave>(v.x);
-    v.y = lanes_sum<kWave>(v.y);
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
-    __syncthreads();
-    v = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < kWide / kWave; ++w) {
-        v.x += lds[w].x;
-        v.y += lds[w].y;
-    }
-    return v;
-}
-
 template <typename T>
 __global__ __launch_bounds__(kWide) void norm_wide_kernel(NormArgs a) {
     __shared__ float2 lds[kWide / kWave];
@@ -477,17 +400,6 @@ __global__ __launch_bounds__(kBlock) void norm_wide_sums_kernel(NormArgs a) {
     a.partial[((int64_t)blockIdx.y * 2 + 1) * a.d + c] = gb;
 }
 
-// How a row is held: lanes per row, vectors per lane (0: not in registers).  A lane has at most 16 columns, whose gradients of weight and bias take as many registers each.
-struct NormShape { int lpr, k; };
-static NormShape norm_shape(int64_t d, int vec) {
-    const int64_t nv = (d + vec - 1) / vec;
-    int lpr = 2;
-    while (lpr < kWave && lpr < nv) lpr *= 2;
-    if (nv <= (16 / vec) * kWave) return {lpr, (int)((nv + kWave - 1) / kWave)};
-    if (nv <= 256) return {256, 1};
-    return nv <= 512 ? NormShape{256, 2} : nv <= 1024 ? NormShape{1024, 1} : nv <= 2048 && vec == 4 ? NormShape{1024, 2} : NormShape{1024, 0};
-}
-
 typedef void (*norm_kernel_t)(NormArgs);
 // Workgroups that take `rows` rows each, whatever a launch holds.
 template <typename T>
@@ -508,38 +420,10 @@ static int launch_rows(norm_kernel_t kernel, const NormArgs &a, int64_t rows, in
         hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3((unsigned)threads), 0, s, part);
     });
 }
-template <typename T, template <int, int> class F>
-static norm_kernel_t norm_pick(NormShape s) {
-    switch (s.lpr) {
-    case 2: return F<2, 1>::kernel;
-    case 4: return F<4, 1>::kernel;
-    case 8: return F<8, 1>::kernel;
-    case 16: return F<16, 1>::kernel;
-    case 32: return F<32, 1>::kernel;
-    case 64:
-        if constexpr (kVec<T> == 4) {
-            if (s.k > 2) return s.k == 3 ? (norm_kernel_t)F<64, 3>::kernel : (norm_kernel_t)F<64, 4>::kernel;
-        }
-        return s.k == 1 ? (norm_kernel_t)F<64, 1>::kernel : (norm_kernel_t)F<64, 2>::kernel;
-    case 256:
-        if constexpr (kVec<T> == 8) {
-            if (s.k == 1) return F<256, 1>::kernel;
-        }
-        return F<256, 2>::kernel;
-    default:
-        if constexpr (kVec<T> == 4) {
-            if (s.k == 2) return F<1024, 2>::kernel;
-        }
-        return F<1024, 1>::kernel;
-    }
-}
 // Rows one after the other that a lane requests at once.  Forward: 16 columns' worth, against 8: 65536 x 512 fp32 43.5 us and 45.4, 232965 x 128 bf16 21.3 and 22.0, 56944 x 251 bf16 15.3
 // and 17.3, but 232965 x 128 fp32 40.4 and 39.7, 370000 x 64 fp32 34.0 and 33.2.
 constexpr int norm_rows(int lpr, int k, int vec) { return lpr > kWave || k * vec >= 16 ? 1 : 16 / (k * vec); }
 constexpr int norm_grad_rows(int lpr, int k) { return lpr <= kWave && k == 1 ? 2 : 1; }
-// Threads of a workgroup, and the rows that it takes side by side.
-static int norm_block(NormShape s, bool backward) { return s.lpr <= kWave ? (backward ? 2 * kBlock : kBlock) : s.lpr; }
-static int64_t norm_side(NormShape s, bool backward) { return norm_block(s, backward) / s.lpr; }
 template <typename T, bool TAIL>
 struct Forward {
     template <int LPR, int K>
@@ -598,7 +482,7 @@ int hag_layer_norm(int64_t n, int64_t d, hag_dtype_t dtype, const void *x, int64
         using T = decltype(e);
         const NormShape s = norm_shape(d, kVec<T>);
         if (s.k == 0) return launch_rows<T>(norm_wide_kernel<T>, a, 1, kWide, (hipStream_t)stream);
-        const norm_kernel_t kernel = d % kVec<T> ? norm_pick<T, Forward<T, true>::template Of>(s) : norm_pick<T, Forward<T, false>::template Of>(s);
+        const norm_kernel_t kernel = d % kVec<T> ? norm_pick<norm_kernel_t, T, Forward<T, true>::template Of>(s) : norm_pick<norm_kernel_t, T, Forward<T, false>::template Of>(s);
         return launch_rows<T>(kernel, a, norm_side(s, false) * norm_rows(s.lpr, s.k, kVec<T>), norm_block(s, false), (hipStream_t)stream);
     });
 }
@@ -648,7 +532,7 @@ int hag_layer_norm_grad(int64_t n, int64_t d, hag_dtype_t dtype, const void *g_y
             if (params) hipLaunchKernelGGL(norm_wide_sums_kernel<T>, dim3((unsigned)((d + kWave - 1) / kWave), (unsigned)groups), dim3(kBlock), 0, s, a);
         } else {
             const size_t lds = shape.lpr <= kWave ? (size_t)(norm_block(shape, true) / kWave) * shape.lpr * shape.k * kVec<T> * 2 * sizeof(float) : 0;
-            const norm_kernel_t kernel = d % kVec<T> ? norm_pick<T, Backward<T, true>::template Of>(shape) : norm_pick<T, Backward<T, false>::template Of>(shape);
+            const norm_kernel_t kernel = d % kVec<T> ? norm_pick<norm_kernel_t, T, Backward<T, true>::template Of>(shape) : norm_pick<norm_kernel_t, T, Backward<T, false>::template Of>(shape);
             hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)norm_block(shape, true)), lds, s, a);
         }
         HIP_TRY(hipGetLastError());
