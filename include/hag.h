@@ -442,6 +442,61 @@ typedef struct hag_tensor {
 size_t hag_clip_workspace_bytes(int64_t tensors);
 int hag_clip_gradients(int64_t tensors, const hag_tensor_t *list, double max_norm, float *norm, void *workspace, void *stream);
 
+/* What makes a model of many layers trainable and cheap to serve.  As above: device pointers, kernels only, elements HAG_F32, HAG_BF16 or HAG_F16 at any address that suits one element,
+ * sums and statistics in fp32 or wider, fixed order of additions, inputs with contiguous rows and a row stride in elements, outputs contiguous unless they have a stride, and apart
+ * from the inputs in memory; n is below 2^31, d is in 1 .. 2^20.
+ *
+ * hag_rms_norm: h = x + residual (rounded to the elements' type; what follows takes it as it was rounded), rstd = 1 / sqrt(mean of h^2 + eps) per row, y = h * rstd * weight.  residual
+ * may be NULL: h = x, and nothing is written to `h`.  weight [d] of the type of x or HAG_F32, or NULL: 1; rstd [n] may be NULL: not kept.  Finite rows of any size; rstd is an fp32
+ * number (rows below 1e-38 take an eps); rows of zeros without an eps give NaN.
+ * hag_rms_norm_fp8: the same with y in 8 bits: codes, e4m3 elements (448 the largest, 0x7f no number), and one power of two for every 32 columns, scales [n, ceil(d / 32)], a byte s for
+ * 2^(s - 127): the smallest that leaves the block's largest amount at most 448, 127 for a block of zeros; elements are rounded to the nearest.  What is no finite number becomes
+ * 0x7f and leaves its block's scale alone.  Columns of the output beyond d are left as they were.
+ * hag_rms_norm_grad: g_x, the gradient at x and at the residual, and g_weight (of param_dtype; may be NULL: not wanted) of a loss whose gradient at y is g_y and, along another way, at h is
+ * g_h (may be NULL: none); rstd as the forward call left it.
+ *
+ * hag_fp8_product: y [n, k] = x w^T for x [n, d] and w [k, d] in 8 bits, with scales as above (255: no number) and strides in bytes; k at most 2^20; y of `dtype`, summed in fp32.  For
+ * HAG_F32 products are exact (elements that are with their scale below 2^-126 may count as 0, above 2^128 as infinite); for 16 bits a product may be cut off at 2^-14 of the largest
+ * of 8 or 16 neighbours, as the matrix cores do.  `workspace` of hag_fp8_product_workspace_bytes(n, d, k) bytes, 16-byte aligned (may be NULL where that is 0).
+ *
+ * hag_adamw: one step, in place, of
+ *   g' = c g, m = beta1 m + (1 - beta1) g', v = beta2 v + (1 - beta2) g'^2, p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
+ * for every element of every tensor; c = min(1, max_norm / *norm) with a norm (fp32, device), 1 without.  A norm that is no finite number leaves everything as it is.  Parameters of
+ * 16 bits are rounded once a step; `copy` (may be NULL) gets the new parameters in copy_dtype: 16 bits to compute with beside HAG_F32 ones that are trained.  Gradients of HAG_F32
+ * parameters may be of any type, of others are of theirs.  bits 32: m and v are fp32.  bits 8: m and, in the place of v, its root, both in 8 bits as above, in blocks of 32 consecutive
+ * elements; they are rounded up or down by chance, so that their mean is kept, by a hash of seed, step and the element's number in its tensor: the same call gives the same bits.
+ * Squares of gradients are taken in fp32: they count up to 1e19.  `list` is host memory, read during the call.  lr_device (fp32) and step_device (HAG_I64, at least 1; both may be NULL) take
+ * the place of lr and step, for calls that are captured and replayed.  Tensors must not overlap. */
+int hag_rms_norm(int64_t n, int64_t d, hag_dtype_t dtype, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, hag_dtype_t param_dtype, const void *weight,
+                 float eps, void *h, void *y, float *rstd, void *stream);
+int hag_rms_norm_fp8(int64_t n, int64_t d, hag_dtype_t dtype, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, hag_dtype_t param_dtype, const void *weight,
+                     float eps, void *h, uint8_t *codes, int64_t codes_stride, uint8_t *scales, int64_t scales_stride, void *stream);
+size_t hag_rms_norm_grad_workspace_bytes(int64_t n, int64_t d);
+int hag_rms_norm_grad(int64_t n, int64_t d, hag_dtype_t dtype, const void *g_y, int64_t g_y_stride, const void *g_h, int64_t g_h_stride, const void *h, int64_t h_stride,
+                      hag_dtype_t param_dtype, const void *weight, const float *rstd, void *g_x, void *g_weight, void *workspace, void *stream);
+size_t hag_fp8_product_workspace_bytes(int64_t n, int64_t d, int64_t k);
+int hag_fp8_product(int64_t n, int64_t d, int64_t k, const uint8_t *x, int64_t x_stride, const uint8_t *x_scales, int64_t x_scales_stride, const uint8_t *w, int64_t w_stride,
+                    const uint8_t *w_scales, int64_t w_scales_stride, hag_dtype_t dtype, void *y, void *workspace, void *stream);
+typedef struct hag_adamw_tensor {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    void *copy;
+    uint8_t *m_scales, *v_scales;                            /* bits 8: ceil(count / 32) bytes each */
+    int64_t count;                                           /* elements */
+    int32_t param_dtype, grad_dtype, copy_dtype, zero;       /* zero: 0 */
+} hag_adamw_tensor_t;
+typedef struct hag_adamw_options {
+    double lr, beta1, beta2, eps, weight_decay, max_norm;
+    int64_t step;
+    const float *lr_device;
+    const int64_t *step_device;
+    const float *norm;
+    uint32_t seed;
+    int32_t bits;
+} hag_adamw_options_t;
+int hag_adamw(int64_t tensors, const hag_adamw_tensor_t *list, const hag_adamw_options_t *options, void *stream);
+
 /* Algorithmic bytes one call moves (every HAG edge one row read, every produced
  * row one write, plus index reads), for roofline accounting.  which: 0 hag_forward,
  * 1 hag_backward, 2 hag_naive_forward, 3 hag_naive_backward. */

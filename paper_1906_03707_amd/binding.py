@@ -39,6 +39,7 @@ EXPORTS = [
     "hag_weight_grad_workspace_bytes", "hag_weight_grad", "hag_narrow_product", "hag_softmax_loss_workspace_bytes", "hag_softmax_loss", "hag_softmax_loss_grad",
     "hag_embedding", "hag_embedding_grad_workspace_bytes", "hag_embedding_grad", "hag_layer_norm", "hag_layer_norm_grad_workspace_bytes", "hag_layer_norm_grad",
     "hag_clip_workspace_bytes", "hag_clip_gradients",
+    "hag_rms_norm", "hag_rms_norm_fp8", "hag_rms_norm_grad_workspace_bytes", "hag_rms_norm_grad", "hag_fp8_product_workspace_bytes", "hag_fp8_product", "hag_adamw",
 ]
 ROUTES = ("hag", "lists", "component_hag", "component_lists", "dense", "one_launch", "scatter")   # HAG_ROUTE_*
 HAG_STATIC_SCRATCH_BYTES = 64 << 20
@@ -48,6 +49,11 @@ class HagError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"libhag error {code}: {msg}")
         self.code = code
+
+
+class hag_adamw_options_t(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_double) for k in ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm")] + [("step", ctypes.c_int64)]
+                + [(k, ctypes.c_void_p) for k in ("lr_device", "step_device", "norm")] + [("seed", ctypes.c_uint32), ("bits", ctypes.c_int32)])
 
 
 class hag_stats_t(ctypes.Structure):
@@ -141,6 +147,15 @@ def lib():
         L.hag_clip_workspace_bytes.argtypes = [i64]
         L.hag_clip_workspace_bytes.restype = size_t
         L.hag_clip_gradients.argtypes = [i64, vp, ctypes.c_double, vp, vp, vp]
+        L.hag_rms_norm.argtypes = [i64, i64, i32, vp, i64, vp, i64, i32, vp, f32, vp, vp, vp, vp]
+        L.hag_rms_norm_fp8.argtypes = [i64, i64, i32, vp, i64, vp, i64, i32, vp, f32, vp, vp, i64, vp, i64, vp]
+        L.hag_rms_norm_grad_workspace_bytes.argtypes = [i64, i64]
+        L.hag_rms_norm_grad_workspace_bytes.restype = size_t
+        L.hag_rms_norm_grad.argtypes = [i64, i64, i32, vp, i64, vp, i64, vp, i64, i32] + [vp] * 6
+        L.hag_fp8_product_workspace_bytes.argtypes = [i64, i64, i64]
+        L.hag_fp8_product_workspace_bytes.restype = size_t
+        L.hag_fp8_product.argtypes = [i64, i64, i64] + [vp, i64] * 4 + [i32] + [vp] * 3
+        L.hag_adamw.argtypes = [i64, vp, ctypes.POINTER(hag_adamw_options_t), vp]
         _lib = L
     return _lib
 
@@ -671,6 +686,197 @@ def clip_gradients(tensors, max_norm, out=None):
     if rc != 0:
         _check(rc)
     return norm
+
+
+def _norm_input(x, weight, residual):
+    """(element code, row stride, residual's address and row stride, code and address of the weight) of an RMS norm's arguments."""
+    device = _device()
+    code, stride = _rows("x", x, device)
+    param_code, (w, _) = _norm_params(x, weight, None)
+    if residual is None:
+        return code, stride, None, 0, param_code, w
+    res_code, res_stride = _rows("residual", residual, device)
+    if res_code != code or residual.shape != x.shape:
+        raise ValueError(f"residual must match x: {x.dtype} {tuple(x.shape)}, got {residual.dtype} {tuple(residual.shape)}")
+    return code, stride, residual.data_ptr(), res_stride, param_code, w
+
+
+def rms_norm(x, weight=None, eps=1e-5, residual=None):
+    """(y, h, rstd) of x [n, d]: h = x + residual (x itself without one), rstd = 1 / sqrt(mean of h^2 + eps) of every row, y = h * rstd * weight (hag_rms_norm)."""
+    import torch
+    code, stride, res, res_stride, param_code, w = _norm_input(x, weight, residual)
+    n, d = x.shape
+    y, rstd = x.new_empty((n, d)), x.new_empty(n, dtype=None if code == HAG_F32 else torch.float32)
+    h = x if residual is None else x.new_empty((n, d))
+    rc = lib().hag_rms_norm(n, d, code, x.data_ptr(), stride, res, res_stride, param_code, w, eps, h.data_ptr(), y.data_ptr(), rstd.data_ptr(), _raw_stream())
+    if rc != 0:
+        _check(rc)
+    return y, h, rstd
+
+
+def rms_norm_fp8(x, weight=None, eps=1e-5, residual=None):
+    """(codes, scales, h): rms_norm with y in 8 bits, codes [n, d] float8_e4m3fn, whose rows begin at multiples of 16 elements, and scales [n, ceil(d / 32)] float8_e8m0fnu, a power of two
+    for every 32 columns: y is about codes * scales (hag_rms_norm_fp8)."""
+    import torch
+    code, stride, res, res_stride, param_code, w = _norm_input(x, weight, residual)
+    n, d = x.shape
+    wide, blocks = (d + 15) // 16 * 16, (d + 31) // 32
+    codes, scales = x.new_empty((n, wide), dtype=torch.float8_e4m3fn), x.new_empty((n, blocks), dtype=torch.float8_e8m0fnu)
+    h = x if residual is None else x.new_empty((n, d))
+    rc = lib().hag_rms_norm_fp8(n, d, code, x.data_ptr(), stride, res, res_stride, param_code, w, eps, h.data_ptr(), codes.data_ptr(), wide, scales.data_ptr(), blocks, _raw_stream())
+    if rc != 0:
+        _check(rc)
+    return codes if wide == d else codes[:, :d], scales, h
+
+
+def rms_norm_grad(g_y, h, rstd, weight=None, g_h=None, params=True):
+    """(g_x, g_weight): the gradients of rms_norm for the gradient g_y at y and, where h is used further, g_h at h; h and rstd as it returned them.  g_x is the gradient at x
+    and at the residual; g_weight has the type of weight (float32 without one), None if not params (hag_rms_norm_grad)."""
+    device = _device()
+    code, stride = _rows("h", h, device)
+    n, d = h.shape
+    more = [None, 0]
+    g_code, g_stride = _rows("g_y", g_y, device)
+    if g_code != code or g_y.shape != h.shape:
+        raise ValueError(f"g_y must match h: {h.dtype} {tuple(h.shape)}, got {g_y.dtype} {tuple(g_y.shape)}")
+    if g_h is not None:
+        more_code, more_stride = _rows("g_h", g_h, device)
+        if more_code != code or g_h.shape != h.shape:
+            raise ValueError(f"g_h must match h: {h.dtype} {tuple(h.shape)}, got {g_h.dtype} {tuple(g_h.shape)}")
+        more = [g_h.data_ptr(), more_stride]
+    if _elements.get(rstd.dtype) != HAG_F32 or rstd.shape != (n,) or rstd.get_device() != device or not rstd.is_contiguous():
+        raise ValueError(f"rstd must be contiguous float32, one for each of the {n} rows, on the current device")
+    param_code, (w, _) = _norm_params(h, weight, None)
+    g_x, g_w, ws, where = h.new_empty((n, d)), None, None, (None, None)
+    L = lib()
+    if params:
+        g_w, ws = (rstd if weight is None else weight).new_empty(d), rstd.new_empty(L.hag_rms_norm_grad_workspace_bytes(n, d) // 4)
+        where = g_w.data_ptr(), ws.data_ptr()
+    rc = L.hag_rms_norm_grad(n, d, code, g_y.data_ptr(), g_stride, *more, h.data_ptr(), stride, param_code, w, rstd.data_ptr(), g_x.data_ptr(), *where, _raw_stream())
+    if rc != 0:
+        _check(rc)
+    return g_x, g_w
+
+
+def _rows_fp8(name, codes, scales, device):
+    """Row strides of rows in 8 bits and of their scales."""
+    import torch
+    if codes.dtype != torch.float8_e4m3fn or scales.dtype != torch.float8_e8m0fnu or codes.dim() != 2 or codes.get_device() != device or scales.get_device() != device:
+        raise ValueError(f"{name} must be a float8_e4m3fn matrix with float8_e8m0fnu scales on the current device, got {codes.dtype} {tuple(codes.shape)} on {codes.device} "
+                         f"and {scales.dtype} on {scales.device}")
+    n, d = codes.shape
+    if scales.shape != (n, (d + 31) // 32):
+        raise ValueError(f"the scales of {name} {(n, d)} must have shape {(n, (d + 31) // 32)}, got {tuple(scales.shape)}")
+    if (codes.stride(1) != 1 and d > 1 or scales.stride(1) != 1 and d > 32) and n > 0:
+        raise ValueError(f"the rows of {name} and its scales must be contiguous, got strides {tuple(codes.stride())} and {tuple(scales.stride())}")
+    return (codes.stride(0), scales.stride(0)) if n > 1 else (d, scales.shape[1])
+
+
+def fp8_product(x, x_scales, w, w_scales, dtype=None):
+    """x w^T [n, k] of rows in 8 bits, x [n, d] and w [k, d] as rms_norm_fp8 and quantize_fp8 give them; dtype: float32 (the default), bfloat16 or float16 (hag_fp8_product)."""
+    import torch
+    device = _device()
+    dtype = torch.float32 if dtype is None else dtype
+    code = (_elements or _element_codes()).get(dtype)
+    if code is None:
+        raise ValueError(f"unsupported dtype {dtype}")
+    x_strides, w_strides = _rows_fp8("x", x, x_scales, device), _rows_fp8("w", w, w_scales, device)
+    (n, d), k = x.shape, w.shape[0]
+    if w.shape[1] != d:
+        raise ValueError(f"x {tuple(x.shape)} and w {tuple(w.shape)} do not match")
+    L = lib()
+    y, nbytes = x.new_empty((n, k), dtype=dtype), L.hag_fp8_product_workspace_bytes(n, d, k)
+    ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    rc = L.hag_fp8_product(n, d, k, x.data_ptr(), x_strides[0], x_scales.data_ptr(), x_strides[1], w.data_ptr(), w_strides[0], w_scales.data_ptr(), w_strides[1], code, y.data_ptr(),
+                           ws.data_ptr() if nbytes else None, _raw_stream())
+    if rc != 0:
+        _check(rc)
+    return y
+
+
+def adamw_states(params, bits=32):
+    """States of adamw for the tensors `params` that have seen no gradient: {"m": ..., "v": ...}, lists of tensors of zeros, float32 for 32 bits and float8_e4m3fn for 8, then with
+    "m_scales" and "v_scales", float8_e8m0fnu, one for every 32 elements in the order of memory."""
+    import torch
+    if bits not in (8, 32):
+        raise ValueError("states have 32 or 8 bits")
+    dtype = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    # (their elements are in the order of the parameter's memory: what shape they have says nothing)
+    states = {k: [torch.zeros(p.numel(), dtype=torch.float32 if bits == 32 else torch.uint8, device=p.device).view(dtype) for p in params] for k in ("m", "v")}
+    if bits == 8:
+        states.update({k: [torch.full(((p.numel() + 31) // 32,), 127, dtype=torch.uint8, device=p.device).view(torch.float8_e8m0fnu) for p in params] for k in ("m_scales", "v_scales")})
+    return states
+
+
+def _scalar_at(name, t, dtype, device):
+    if t.numel() != 1 or t.dtype != dtype or t.get_device() != device:
+        raise ValueError(f"{name} must be one {dtype} on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def adamw(params, grads, m, v, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, norm=None, max_norm=None, copies=None, m_scales=None, v_scales=None, seed=0):
+    """One step of AdamW on the tensors `params`, in place, with their gradients and states, lists of one tensor each (hag_adamw).
+
+    params float32, bfloat16 or float16, dense; gradients of the same shape and order in memory and, but for float32 parameters, type.  m and v as adamw_states makes them, with
+    m_scales and v_scales for 8 bits.  step: a number, from 1 on, or an int64 scalar on the device; lr: a number or a float32 scalar on the device.  With norm (a float32 scalar on the
+    device, as clip_gradients returns it) the gradients count as if scaled down to max_norm where it is above, and nothing changes where it is no finite number.  copies: tensors (or
+    None) of any of the three types that get the new parameters too.  seed: of the rounding of 8-bit states."""
+    import torch
+    device, codes = _device(), _elements or _element_codes()
+    bits = 32 if m_scales is None else 8
+    params, grads = list(params), list(grads)
+    lists = [list(x) for x in ((m, v) if bits == 32 else (m, v, m_scales, v_scales if v_scales is not None else ()))]
+    if any(len(x) != len(params) for x in (grads, *lists)) or (copies is not None and len(copies) != len(params)) or (m_scales is None and v_scales is not None):
+        raise ValueError(f"{len(params)} parameters need as many gradients, states, scales of 8-bit states and copies")
+    options = hag_adamw_options_t(0.0, betas[0], betas[1], eps, weight_decay, 1.0, 0, None, None, None, seed & 0xFFFFFFFF, bits)
+    if isinstance(step, torch.Tensor):
+        options.step_device = _scalar_at("step", step, torch.int64, device)
+    else:
+        options.step = step
+    if isinstance(lr, torch.Tensor):
+        options.lr_device = _scalar_at("lr", lr, torch.float32, device)
+    else:
+        options.lr = lr
+    if (norm is None) != (max_norm is None):
+        raise ValueError("norm and max_norm go together")
+    if norm is not None:
+        options.norm, options.max_norm = _scalar_at("norm", norm, torch.float32, device), max_norm
+    state_dtype = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    entries, written = [], []
+    for i, (p, g) in enumerate(zip(params, grads)):
+        code, g_code, whole, count = codes.get(p.dtype), codes.get(g.dtype), p.is_contiguous(), p.numel()
+        if code is None or p.get_device() != device or not (whole or _dense(p)):
+            raise ValueError(f"dense float32, bfloat16 or float16 parameters on the current device are needed, got {p.dtype} {tuple(p.shape)} with strides {tuple(p.stride())} on {p.device}")
+        if g_code is None or (g_code != code and code != HAG_F32) or g.shape != p.shape or g.get_device() != device or not (whole and g.is_contiguous() or g.stride() == p.stride()):
+            raise ValueError(f"a gradient must match its parameter: {p.dtype} {tuple(p.shape)} with strides {tuple(p.stride())}, got {g.dtype} {tuple(g.shape)} with {tuple(g.stride())}")
+        at = [p.data_ptr(), g.data_ptr()]
+        for x in lists[:2]:
+            t = x[i]
+            if t.dtype != state_dtype or t.numel() != count or t.get_device() != device or not (t.is_contiguous() or t.shape == p.shape and t.stride() == p.stride()):
+                raise ValueError(f"a state must be {state_dtype}, dense, of its parameter's {count} elements, on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+            at.append(t.data_ptr())
+        copy, copy_code = copies[i] if copies is not None else None, 0
+        if copy is not None:
+            copy_code = codes.get(copy.dtype)
+            if copy_code is None or copy.shape != p.shape or copy.get_device() != device or not (whole and copy.is_contiguous() or copy.stride() == p.stride()):
+                raise ValueError(f"a copy must match its parameter {tuple(p.shape)} with strides {tuple(p.stride())}, got {copy.dtype} {tuple(copy.shape)} with {tuple(copy.stride())}")
+        at.append(0 if copy is None else copy.data_ptr())
+        for x in lists[2:]:
+            t = x[i]
+            if t.dtype != torch.float8_e8m0fnu or t.numel() != (count + 31) // 32 or t.get_device() != device or not t.is_contiguous():
+                raise ValueError(f"scales must be contiguous float8_e8m0fnu, {(count + 31) // 32} of them, on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+            at.append(t.data_ptr())
+        if bits == 32:
+            at += (0, 0)
+        if count:
+            written += [x for x in (at[0], *at[2:]) if x]
+            entries += (*at, count, code | g_code << 32, copy_code)
+    if len(set(written)) != len(written):
+        raise ValueError("a tensor is named twice")
+    table = array.array("q", entries)
+    rc = lib().hag_adamw(len(entries) // 10, table.buffer_info()[0], ctypes.byref(options), _raw_stream())
+    if rc != 0:
+        _check(rc)
 
 
 def probe_rows(src, n_rows, d, reads, from_lds, workgroups, sink) -> int:
