@@ -24,7 +24,222 @@ typedef __bf16 wide2_t __attribute__((ext_vector_type(2)));
 typedef float sums_t __attribute__((ext_vector_type(4)));
 typedef uint32_t bytes16_t __attribute__((ext_vector_type(4), aligned(1)));
 
-// 16 columns from `col` of a row, zeros from column d on
+// The scale of a block, 1 beyond the last
+__device__ __forceinline__ uint32_t load_scale(const uint8_t *row, int block, int d) { return block * kScaleBlock < d ? row[block] : 127u; }
+
+// 128 columns of a row, as far as a lane brings them: two pieces of 16, in the types of the instruction
+template <bool WIDE>
+struct Part;
+template <>
+struct Part<false> {
+    frag_t f;
+    int scale;
+    Part() = default;
+    // scales: of the lane's blocks in its bytes, the one of columns 32 q first
+    __device__ __forceinline__ Part(const bytes16_t &a, const bytes16_t &b, uint32_t scales) : scale((int)scales) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[i] = (int)a[i]; f[i + 4] = (int)b[i]; }
+    }
+};
+template <>
+struct Part<true> {
+    wide_t f[4];
+    Part() = default;
+    // scales: of the two pieces in the two lower bytes
+    __device__ __forceinline__ Part(const bytes16_t &a, const bytes16_t &b, uint32_t scales) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const float scale = __uint_as_float((half ? scales >> 8 & 0xffu : scales & 0xffu) << 23);   // (only its exponent counts)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t v = half ? b[i] : a[i];
+                const wide2_t low = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, scale, false), high = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, scale, true);
+                wide_t &to = f[half * 2 + i / 2];
+                to[i % 2 * 4] = low.x;
+                to[i % 2 * 4 + 1] = low.y;
+                to[i % 2 * 4 + 2] = high.x;
+                to[i % 2 * 4 + 3] = high.y;
+            }
+        }
+    }
+};
+// A lane's scales out of the four of 128 columns
+template <bool WIDE>
+__device__ __forceinline__ uint32_t lane_scales(uint32_t four, int q) {
+    if (!WIDE) return four >> 8 * q;
+    const uint32_t mine = four >> 8 * (q / 2);             // blocks q / 2 and q / 2 + 2
+    return (mine & 0xffu) | (mine >> 8 & 0xff00u);
+}
+
+// acc[0 .. T) += w x for the T pieces of w; one instruction's sums are not waited for by the next
+template <int T>
+__device__ __forceinline__ void multiply(const Part<false> (&w)[T], const Part<false> &x, sums_t (&acc)[T]) {
+#pragma unroll
+    for (int t = 0; t < T; ++t) acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[t].f, x.f, acc[t], 0, 0, 0, w[t].scale, 0, x.scale);
+}
+template <int T>
+__device__ __forceinline__ void multiply(const Part<true> (&w)[T], const Part<true> &x, sums_t (&acc)[T]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t < T; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[t].f[i], x.f[i], acc[t], 0, 0, 0);
+}
+
+// Columns of y that a lane has of T pieces of w: piece t's row m is column m / 4 * 4 T + 4 t + m % 4 of the 16 T, so that lane q has 4 T adjacent ones, 4 T q and on.
+template <int T>
+__device__ __forceinline__ int piece_column(int t, int m) { return m / 4 * (4 * T) + 4 * t + m % 4; }
+template <typename O, int T>
+__device__ __forceinline__ void store_columns(O *row, int64_t col, int64_t k, const sums_t (&acc)[T]) {
+    constexpr int V = kVec<O>;
+#pragma unroll
+    for (int c = 0; c < 4 * T; c += V) {
+        if (V > 4 * T) break;
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = acc[(c + e) / 4][(c + e) % 4];
+        if (col + c < k) store_vec(row + col + c, (int)min(k - col - c, (int64_t)V), v);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ tiles through LDS
+
+// 16 zeros, for columns beyond the last
+__device__ const uint4 kNoColumns = {0, 0, 0, 0};
+
+// Where piece `chunk` (16 columns) of a row of 128 lies in LDS: lanes that read the same piece of adjacent rows meet different banks.  w is read in the order of piece_column.
+template <bool W>
+__device__ __forceinline__ int placed(int row, int chunk) { return row * 8 + (chunk ^ (W ? (row & 3) | (row >> 4 & 1) << 2 : row & 7)); }
+
+struct ProductTiles {
+    ProductArgs p;
+    int32_t col_tiles, tiles;
+};
+
+// A workgroup takes TM rows of x and TN of w, its wavefronts WR times WC parts of them.  128 columns of both are on their way from memory to LDS while the 128 before are multiplied.
+template <typename O, int TM, int TN, int WR, int WC>
+__global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(ProductTiles args) {
+    constexpr bool WIDE = sizeof(O) == 4;
+    constexpr int THREADS = kWave * WR * WC, ROWS = TM + TN, LOADS = ROWS * 8 / THREADS, X_LOADS = TM * 8 / THREADS, R = TM / WR / 16, T = TN / WC / 16, SCALES = (ROWS + THREADS - 1) / THREADS;
+    static_assert(TM * 8 % THREADS == 0 && ROWS * 8 % THREADS == 0, "a load is of x or of w");
+    // (arrays of their own, and code of its own for either: what is on its way to one is not waited for before the other is read)
+    __shared__ bytes16_t codes0[ROWS * 8] __attribute__((aligned(16))), codes1[ROWS * 8] __attribute__((aligned(16)));
+    __shared__ uint32_t scales0[ROWS], scales1[ROWS];
+    const ProductArgs &a = args.p;
+    // consecutive workgroups go to the 8 XCDs in turn: each XCD gets consecutive tiles, so that the tiles of one set of rows find them in its L2
+    const int share = (args.tiles + 7) / 8, tile = (int)(blockIdx.x % 8) * share + (int)(blockIdx.x / 8);
+    if ((int)(blockIdx.x / 8) >= share || tile >= args.tiles) return;
+    const int64_t row0 = (int64_t)(tile / args.col_tiles) * TM, col0 = (int64_t)(tile % args.col_tiles) * TN;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, r = lane % 16, q = lane / 16, wr = wave / WC, wc = wave % WC;
+    const uint8_t *x = a.x + row0 * a.x_stride, *w = a.w + col0 * a.w_stride;
+    const int x_rows = (int)min(a.n - row0, (int64_t)TM), w_rows = (int)min(a.k - col0, (int64_t)TN), steps = (a.d + 127) / 128, blocks = (a.d + kScaleBlock - 1) / kScaleBlock;
+    uint32_t at[LOADS];                                    // where a thread's pieces begin
+    int chunk[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int slot = i * THREADS + (int)threadIdx.x - (i < X_LOADS ? 0 : TM * 8), row = slot / 8;
+        chunk[i] = i < X_LOADS ? placed<false>(row, slot % 8) % 8 : placed<true>(row, slot % 8) % 8;
+        at[i] = (uint32_t)(i < X_LOADS ? min(row, x_rows - 1) * (uint32_t)a.x_stride : min(row, w_rows - 1) * (uint32_t)a.w_stride) + chunk[i] * 16;
+    }
+    const uint8_t *scale_row[SCALES];
+#pragma unroll
+    for (int i = 0; i < SCALES; ++i) {
+        const int row = min(i * THREADS + (int)threadIdx.x, ROWS - 1);
+        scale_row[i] = row < TM ? a.x_scales + (row0 + min(row, x_rows - 1)) * a.x_scales_stride : a.w_scales + (col0 + min(row - TM, w_rows - 1)) * a.w_scales_stride;
+    }
+    uint32_t scale[SCALES];
+    auto request = [&](int step, bytes16_t *codes) {
+        const uint8_t *from_x = x + (int64_t)step * 128, *from_w = w + (int64_t)step * 128;
+        auto load = [&](const uint8_t *from, int i) {
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)(codes + i * THREADS + wave * kWave), 16, 0, 0);
+        };
+        if ((step + 1) * 128 <= a.d) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) load((i < X_LOADS ? from_x : from_w) + at[i], i);
+        } else {                                           // (a piece that the row ends in is read to its end: it is aligned, so its other bytes are memory too)
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) load(step * 128 + chunk[i] * 16 < a.d ? (i < X_LOADS ? from_x : from_w) + at[i] : (const uint8_t *)&kNoColumns, i);
+        }
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) {
+            typedef uint32_t word_t __attribute__((aligned(1)));
+            if (step * 4 + 4 <= blocks) {
+                scale[i] = *reinterpret_cast<const word_t *>(scale_row[i] + step * 4);
+            } else {
+                scale[i] = 0x7f7f7f7fu;
+#pragma unroll
+                for (int b = 0; b < 3; ++b)
+                    if (step * 4 + b < blocks) scale[i] = (scale[i] & ~(0xffu << 8 * b)) | (uint32_t)scale_row[i][step * 4 + b] << 8 * b;
+            }
+        }
+    };
+    auto keep_scales = [&](uint32_t *scales) {
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i)
+            if (SCALES * THREADS == ROWS || i * THREADS + (int)threadIdx.x < ROWS) scales[i * THREADS + threadIdx.x] = scale[i];
+    };
+    sums_t acc[R][T];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int t = 0; t < T; ++t) acc[i][t] = sums_t{0.f, 0.f, 0.f, 0.f};
+    // what the row's last piece has beyond its end becomes zeros, by the thread that brought it
+    auto cut = [&](int step, bytes16_t *codes) {
+        __builtin_amdgcn_s_waitcnt(0);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int have = a.d - step * 128 - chunk[i] * 16;
+            if (have <= 0 || have >= 16) continue;
+            bytes16_t &v = codes[i * THREADS + threadIdx.x];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) v[b] &= have >= 4 * b + 4 ? ~0u : have <= 4 * b ? 0u : (1u << 8 * (have - 4 * b)) - 1u;
+        }
+    };
+    // (rows 16 apart of x and 4 apart of w, in the order that they are read, have their pieces in the same places)
+    static_assert(T == 4, "pieces of w are placed for 64 columns of a wavefront");
+    const int x_row = wr * (TM / WR) + r, w_row = wc * (TN / WC) + piece_column<T>(0, r);
+    const int x_a = placed<false>(x_row, q), x_b = placed<false>(x_row, q + 4), w_a = TM * 8 + placed<true>(w_row, q), w_b = TM * 8 + placed<true>(w_row, q + 4);
+    auto work = [&](const bytes16_t *of, const uint32_t *four) {
+        Part<WIDE> pw[T];
+#pragma unroll
+        for (int t = 0; t < T; ++t) pw[t] = Part<WIDE>(of[w_a + t * 32], of[w_b + t * 32], lane_scales<WIDE>(four[TM + w_row + t * 4], q));
+        // the next piece of x is requested before the present one is multiplied, and no other: more would not fit the registers
+        bytes16_t a_next = of[x_a], b_next = of[x_b];
+        uint32_t four_next = four[x_row];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const Part<WIDE> px(a_next, b_next, lane_scales<WIDE>(four_next, q));
+            if (i + 1 < R) {
+                a_next = of[x_a + (i + 1) * 128];
+                b_next = of[x_b + (i + 1) * 128];
+                four_next = four[x_row + (i + 1) * 16];
+            }
+            multiply<T>(pw, px, acc[i]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto turn = [&](int step, bytes16_t *codes, uint32_t *scales, bytes16_t *next) {
+        if (step + 1 == steps && a.d % 16) cut(step, codes);
+        keep_scales(scales);
+        __syncthreads();
+        if (step + 1 < steps) request(step + 1, next);
+        work(codes, scales);
+    };
+    request(0, codes0);
+    for (int step = 0; step < steps; step += 2) {
+        turn(step, codes0, scales0, codes1);
+        if (step + 1 < steps) turn(step + 1, codes1, scales1, codes0);
+    }
+    const int64_t col = col0 + wc * (TN / WC) + q * (4 * T);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int row = wr * (TM / WR) + i * 16 + r;
+        if (row < x_rows) store_columns<O, T>((O *)a.y + (row0 + row) * a.k, col, a.k, acc[i]);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ anything else
+
+// 16 columns from `col` of a row at any address, zeros from column d on
 __device__ __forceinline__ bytes16_t load16(const uint8_t *row, int col, int d) {
     bytes16_t v = {};
     if (col + 16 <= d) {
@@ -36,50 +251,11 @@ __device__ __forceinline__ bytes16_t load16(const uint8_t *row, int col, int d) 
     }
     return v;
 }
-// The scale of a block, 1 beyond the last
-__device__ __forceinline__ uint32_t load_scale(const uint8_t *row, int block, int d) { return block * kScaleBlock < d ? row[block] : 127u; }
-
-// 128 columns from `col` of a row, as far as a lane brings them
 template <bool WIDE>
-struct Part;
-template <>
-struct Part<false> {
-    frag_t f;
-    int scale;
-    __device__ __forceinline__ void load(const uint8_t *row, const uint8_t *scales, int col, int q, int d) {
-        const bytes16_t a = load16(row, col + 16 * q, d), b = load16(row, col + 64 + 16 * q, d);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { f[i] = (int)a[i]; f[i + 4] = (int)b[i]; }
-        scale = (int)load_scale(scales, col / kScaleBlock + q, d);
-    }
-};
-template <>
-struct Part<true> {
-    wide_t f[4];
-    __device__ __forceinline__ void load(const uint8_t *row, const uint8_t *scales, int col, int q, int d) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const bytes16_t v = load16(row, col + 64 * half + 16 * q, d);
-            const float scale = __uint_as_float(load_scale(scales, (col + 64 * half + 16 * q) / kScaleBlock, d) << 23);    // (only its exponent counts)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const wide2_t low = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], scale, false), high = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], scale, true);
-                wide_t &to = f[half * 2 + i / 2];
-                to[i % 2 * 4] = low.x;
-                to[i % 2 * 4 + 1] = low.y;
-                to[i % 2 * 4 + 2] = high.x;
-                to[i % 2 * 4 + 3] = high.y;
-            }
-        }
-    }
-};
-__device__ __forceinline__ sums_t multiply(const Part<false> &w, const Part<false> &x, sums_t acc) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.f, x.f, acc, 0, 0, 0, w.scale, 0, x.scale);
-}
-__device__ __forceinline__ sums_t multiply(const Part<true> &w, const Part<true> &x, sums_t acc) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.f[i], x.f[i], acc, 0, 0, 0);
-    return acc;
+__device__ __forceinline__ Part<WIDE> load_part(const uint8_t *row, const uint8_t *scales, int col, int q, int d) {
+    const int block = col / kScaleBlock;
+    const uint32_t s = WIDE ? load_scale(scales, block + q / 2, d) | load_scale(scales, block + 2 + q / 2, d) << 8 : load_scale(scales, block + q, d);
+    return Part<WIDE>(load16(row, col + 16 * q, d), load16(row, col + 64 + 16 * q, d), s);
 }
 
 // A wavefront takes 16 rows of x and 64 of w.
@@ -87,27 +263,34 @@ template <typename O>
 __global__ __launch_bounds__(kBlock) void product_kernel(ProductArgs a) {
     constexpr bool WIDE = sizeof(O) == 4;
     const int lane = threadIdx.x % kWave, r = lane % 16, q = lane / 16;
-    const int64_t row = ((int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave) * 16 + r, col0 = (int64_t)blockIdx.y * 64;
-    const int64_t x_row = min(row, a.n - 1);
+    const int64_t row = ((int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave) * 16 + r, col0 = (int64_t)blockIdx.y * 64, x_row = min(row, a.n - 1);
     sums_t acc[4] = {};
     for (int c = 0; c < a.d; c += 128) {
-        Part<WIDE> x, w;
-        x.load(a.x + x_row * a.x_stride, a.x_scales + x_row * a.x_scales_stride, c, q, a.d);
+        Part<WIDE> w[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const int64_t w_row = min(col0 + t * 16 + r, a.k - 1);
-            w.load(a.w + w_row * a.w_stride, a.w_scales + w_row * a.w_scales_stride, c, q, a.d);
-            acc[t] = multiply(w, x, acc[t]);
+            const int64_t w_row = min(col0 + piece_column<4>(t, r), a.k - 1);
+            w[t] = load_part<WIDE>(a.w + w_row * a.w_stride, a.w_scales + w_row * a.w_scales_stride, c, q, a.d);
         }
+        multiply<4>(w, load_part<WIDE>(a.x + x_row * a.x_stride, a.x_scales + x_row * a.x_scales_stride, c, q, a.d), acc);
     }
-    if (row >= a.n) return;
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t col = col0 + t * 16 + q * 4 + e;
-            if (col < a.k) ((O *)a.y)[row * a.k + col] = (O)acc[t][e];
-        }
+    if (row < a.n) store_columns<O, 4>((O *)a.y + row * a.k, col0 + q * 16, a.k, acc);
+}
+
+template <typename O, int TM, int TN, int WR, int WC>
+static int launch_tiles(const ProductArgs &a, hipStream_t s) {
+    const int64_t col_tiles = (a.k + TN - 1) / TN, row_tiles = (a.n + TM - 1) / TM, most = std::max<int64_t>(1, ((int64_t)1 << 20) / col_tiles);
+    for (int64_t first = 0; first < row_tiles; first += most) {
+        const int64_t rows = std::min(most, row_tiles - first), at = first * TM;
+        ProductTiles t = {a, (int32_t)col_tiles, (int32_t)(rows * col_tiles)};
+        t.p.x += at * a.x_stride;
+        t.p.x_scales += at * a.x_scales_stride;
+        t.p.y = (O *)a.y + at * a.k;
+        t.p.n = std::min(rows * TM, a.n - at);
+        hipLaunchKernelGGL((product_tile_kernel<O, TM, TN, WR, WC>), dim3((unsigned)((t.tiles + 7) / 8 * 8)), dim3(kWave * WR * WC), 0, s, t);
+        HIP_TRY(hipGetLastError());
+    }
+    return HAG_OK;
 }
 
 }  // namespace hag
@@ -126,15 +309,19 @@ int hag_fp8_product(int64_t n, int64_t d, int64_t k, const uint8_t *x, int64_t x
     if (n == 0 || k == 0) return HAG_OK;
     if (!x || !x_scales || !w || !w_scales || !y) { set_error("NULL pointer"); return HAG_EINVAL; }
     const ProductArgs a = {x, w, x_scales, w_scales, x_stride, w_stride, x_scales_stride, w_scales_stride, n, k, (int32_t)d, y};
+    // the loads to LDS take pieces of 16 bytes at multiples of 16, and rows of a tile at 32-bit distances
+    const bool aligned = !(((uintptr_t)x | (uintptr_t)w | (uintptr_t)x_stride | (uintptr_t)w_stride) & 15) && x_stride < (1 << 23) && w_stride < (1 << 23);
     return elem_switch(dtype, [&](auto e) {
         using O = decltype(e);
+        hipStream_t s = (hipStream_t)stream;
+        if (aligned && n > 64) return n * k >= (int64_t)1 << 24 && k > 128 ? (sizeof(O) == 2 ? launch_tiles<O, 256, sizeof(O) == 2 ? 256 : 128, sizeof(O) == 2 ? 2 : 4, sizeof(O) == 2 ? 4 : 2>(a, s) : launch_tiles<O, 256, 128, 4, 2>(a, s)) : launch_tiles<O, 128, 128, 2, 2>(a, s);
         return launch_parts((n + 63) / 64, kBlock, [&](int64_t first, int64_t count) {
             ProductArgs part = a;
             part.x += first * 64 * x_stride;
             part.x_scales += first * 64 * x_scales_stride;
             part.y = (O *)a.y + first * 64 * k;
             part.n = std::min(count * 64, n - first * 64);
-            hipLaunchKernelGGL(product_kernel<O>, dim3((unsigned)count, (unsigned)((k + 63) / 64)), dim3(kBlock), 0, (hipStream_t)stream, part);
+            hipLaunchKernelGGL(product_kernel<O>, dim3((unsigned)count, (unsigned)((k + 63) / 64)), dim3(kBlock), 0, s, part);
         });
     });
 }
