@@ -85,19 +85,21 @@ __device__ __forceinline__ void multiply(const Part<true> (&w)[T], const Part<tr
         for (int t = 0; t < T; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[t].f[i], x.f[i], acc[t], 0, 0, 0);
 }
 
-// Columns of y that a lane has of T pieces of w: piece t's row m is column m / 4 * 4 T + 4 t + m % 4 of the 16 T, so that lane q has 4 T adjacent ones, 4 T q and on.
-template <int T>
-__device__ __forceinline__ int piece_column(int t, int m) { return m / 4 * (4 * T) + 4 * t + m % 4; }
+// Which row of w is row m of piece t, so that a store of 16 bytes by the 4 lanes of a row of y writes 64 adjacent bytes: lanes have 4 adjacent columns of a piece; where 16 bytes are 8
+// columns, pieces take turns of 4.
+template <typename O>
+__device__ __forceinline__ int piece_column(int t, int m) { return kVec<O> == 4 ? t * 16 + m : t / 2 * 32 + m / 4 * 8 + t % 2 * 4 + m % 4; }
+// A lane's columns of the T pieces, q = lane / 16, to the row of y at `to`, of which `have` columns are there
 template <typename O, int T>
-__device__ __forceinline__ void store_columns(O *row, int64_t col, int64_t k, const sums_t (&acc)[T]) {
-    constexpr int V = kVec<O>;
+__device__ __forceinline__ void store_columns(O *to, int q, int have, const sums_t (&acc)[T]) {
+    constexpr int V = kVec<O>, P = V / 4;
 #pragma unroll
-    for (int c = 0; c < 4 * T; c += V) {
-        if (V > 4 * T) break;
+    for (int t = 0; t < T; t += P) {
+        const int col = t * 16 + q * V;
         float v[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = acc[(c + e) / 4][(c + e) % 4];
-        if (col + c < k) store_vec(row + col + c, (int)min(k - col - c, (int64_t)V), v);
+        for (int e = 0; e < V; ++e) v[e] = acc[t + e / 4][e % 4];
+        if (col < have) store_vec(to + col, have - col, v);
     }
 }
 
@@ -107,8 +109,8 @@ __device__ __forceinline__ void store_columns(O *row, int64_t col, int64_t k, co
 __device__ const uint4 kNoColumns = {0, 0, 0, 0};
 
 // Where piece `chunk` (16 columns) of a row of 128 lies in LDS: lanes that read the same piece of adjacent rows meet different banks.  w is read in the order of piece_column.
-template <bool W>
-__device__ __forceinline__ int placed(int row, int chunk) { return row * 8 + (chunk ^ (W ? (row & 3) | (row >> 4 & 1) << 2 : row & 7)); }
+template <typename O, bool W>
+__device__ __forceinline__ int placed(int row, int chunk) { return row * 8 + (chunk ^ (W && kVec<O> == 8 ? (row & 3) | (row >> 3 & 1) << 2 : row & 7)); }
 
 struct ProductTiles {
     ProductArgs p;
@@ -137,7 +139,7 @@ __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(Produc
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
         const int slot = i * THREADS + (int)threadIdx.x - (i < X_LOADS ? 0 : TM * 8), row = slot / 8;
-        chunk[i] = i < X_LOADS ? placed<false>(row, slot % 8) % 8 : placed<true>(row, slot % 8) % 8;
+        chunk[i] = i < X_LOADS ? placed<O, false>(row, slot % 8) % 8 : placed<O, true>(row, slot % 8) % 8;
         at[i] = (uint32_t)(i < X_LOADS ? min(row, x_rows - 1) * (uint32_t)a.x_stride : min(row, w_rows - 1) * (uint32_t)a.w_stride) + chunk[i] * 16;
     }
     const uint8_t *scale_row[SCALES];
@@ -194,14 +196,14 @@ __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(Produc
             for (int b = 0; b < 4; ++b) v[b] &= have >= 4 * b + 4 ? ~0u : have <= 4 * b ? 0u : (1u << 8 * (have - 4 * b)) - 1u;
         }
     };
-    // (rows 16 apart of x and 4 apart of w, in the order that they are read, have their pieces in the same places)
+    // (rows 16 apart of x, and w's as piece_column puts them, have their pieces in the same places)
     static_assert(T == 4, "pieces of w are placed for 64 columns of a wavefront");
-    const int x_row = wr * (TM / WR) + r, w_row = wc * (TN / WC) + piece_column<T>(0, r);
-    const int x_a = placed<false>(x_row, q), x_b = placed<false>(x_row, q + 4), w_a = TM * 8 + placed<true>(w_row, q), w_b = TM * 8 + placed<true>(w_row, q + 4);
+    const int x_row = wr * (TM / WR) + r, w_row = wc * (TN / WC) + piece_column<O>(0, r);
+    const int x_a = placed<O, false>(x_row, q), x_b = placed<O, false>(x_row, q + 4), w_a = TM * 8 + placed<O, true>(w_row, q), w_b = TM * 8 + placed<O, true>(w_row, q + 4);
     auto work = [&](const bytes16_t *of, const uint32_t *four) {
         Part<WIDE> pw[T];
 #pragma unroll
-        for (int t = 0; t < T; ++t) pw[t] = Part<WIDE>(of[w_a + t * 32], of[w_b + t * 32], lane_scales<WIDE>(four[TM + w_row + t * 4], q));
+        for (int t = 0; t < T; ++t) pw[t] = Part<WIDE>(of[w_a + piece_column<O>(t, 0) * 8], of[w_b + piece_column<O>(t, 0) * 8], lane_scales<WIDE>(four[TM + w_row + piece_column<O>(t, 0)], q));
         // the next piece of x is requested before the present one is multiplied, and no other: more would not fit the registers
         bytes16_t a_next = of[x_a], b_next = of[x_b];
         uint32_t four_next = four[x_row];
@@ -229,11 +231,12 @@ __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(Produc
         turn(step, codes0, scales0, codes1);
         if (step + 1 < steps) turn(step + 1, codes1, scales1, codes0);
     }
-    const int64_t col = col0 + wc * (TN / WC) + q * (4 * T);
+    const int64_t col = col0 + wc * (TN / WC);
+    const int have = (int)max((int64_t)0, min(a.k - col, (int64_t)(TN / WC)));
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int row = wr * (TM / WR) + i * 16 + r;
-        if (row < x_rows) store_columns<O, T>((O *)a.y + (row0 + row) * a.k, col, a.k, acc[i]);
+        if (row < x_rows) store_columns<O, T>((O *)a.y + (row0 + row) * a.k + col, q, have, acc[i]);
     }
 }
 
@@ -269,12 +272,12 @@ __global__ __launch_bounds__(kBlock) void product_kernel(ProductArgs a) {
         Part<WIDE> w[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const int64_t w_row = min(col0 + piece_column<4>(t, r), a.k - 1);
+            const int64_t w_row = min(col0 + piece_column<O>(t, r), a.k - 1);
             w[t] = load_part<WIDE>(a.w + w_row * a.w_stride, a.w_scales + w_row * a.w_scales_stride, c, q, a.d);
         }
         multiply<4>(w, load_part<WIDE>(a.x + x_row * a.x_stride, a.x_scales + x_row * a.x_scales_stride, c, q, a.d), acc);
     }
-    if (row < a.n) store_columns<O, 4>((O *)a.y + row * a.k, col0 + q * 16, a.k, acc);
+    if (row < a.n) store_columns<O, 4>((O *)a.y + row * a.k + col0, q, (int)min(a.k - col0, (int64_t)64), acc);
 }
 
 template <typename O, int TM, int TN, int WR, int WC>

@@ -86,7 +86,8 @@ def test_strides_and_addresses(B, n, d, k, pad, start):
     for dtype in (torch.float32, torch.bfloat16):
         y = B.fp8_product(placed(x, pad, start), placed(xs, pad % 7, start % 3), placed(w, pad, start), placed(ws, pad % 5, start), dtype=dtype)
         check(y, x, xs, w, ws, dtype)
-        assert torch.equal(y, B.fp8_product(x, xs, w, ws, dtype=dtype))
+        # (rows at multiples of 16 bytes and others may be added up in another order: either is within the bound, so nothing says that their last bits are the same)
+        check(B.fp8_product(x, xs, w, ws, dtype=dtype), x, xs, w, ws, dtype)
     row = x[:1].expand(n, d), xs[:1].expand(n, xs.shape[1])           # one row throughout
     check(B.fp8_product(*row, w, ws), *row, w, ws, torch.float32)
 
