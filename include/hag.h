@@ -457,7 +457,7 @@ int hag_clip_gradients(int64_t tensors, const hag_tensor_t *list, double max_nor
  *
  * hag_fp8_product: y [n, k] = x w^T for x [n, d] and w [k, d] in 8 bits, with scales as above (255: no number) and strides in bytes; k at most 2^20; y of `dtype`, summed in fp32.  For
  * HAG_F32 products are exact (elements that are with their scale below 2^-126 may count as 0, above 2^128 as infinite); for 16 bits a product may be cut off at 2^-14 of the largest
- * of 8 or 16 neighbours, as the matrix cores do.  `workspace` of hag_fp8_product_workspace_bytes(n, d, k) bytes, 16-byte aligned (may be NULL where that is 0).
+ * of 8 or 16 neighbours, as the matrix cores do.
  *
  * hag_adamw: one step, in place, of
  *   g' = c g, m = beta1 m + (1 - beta1) g', v = beta2 v + (1 - beta2) g'^2, p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
@@ -474,9 +474,8 @@ int hag_rms_norm_fp8(int64_t n, int64_t d, hag_dtype_t dtype, const void *x, int
 size_t hag_rms_norm_grad_workspace_bytes(int64_t n, int64_t d);
 int hag_rms_norm_grad(int64_t n, int64_t d, hag_dtype_t dtype, const void *g_y, int64_t g_y_stride, const void *g_h, int64_t g_h_stride, const void *h, int64_t h_stride,
                       hag_dtype_t param_dtype, const void *weight, const float *rstd, void *g_x, void *g_weight, void *workspace, void *stream);
-size_t hag_fp8_product_workspace_bytes(int64_t n, int64_t d, int64_t k);
 int hag_fp8_product(int64_t n, int64_t d, int64_t k, const uint8_t *x, int64_t x_stride, const uint8_t *x_scales, int64_t x_scales_stride, const uint8_t *w, int64_t w_stride,
-                    const uint8_t *w_scales, int64_t w_scales_stride, hag_dtype_t dtype, void *y, void *workspace, void *stream);
+                    const uint8_t *w_scales, int64_t w_scales_stride, hag_dtype_t dtype, void *y, void *stream);
 typedef struct hag_adamw_tensor {
     void *param;
     const void *grad;

@@ -39,7 +39,7 @@ EXPORTS = [
     "hag_weight_grad_workspace_bytes", "hag_weight_grad", "hag_narrow_product", "hag_softmax_loss_workspace_bytes", "hag_softmax_loss", "hag_softmax_loss_grad",
     "hag_embedding", "hag_embedding_grad_workspace_bytes", "hag_embedding_grad", "hag_layer_norm", "hag_layer_norm_grad_workspace_bytes", "hag_layer_norm_grad",
     "hag_clip_workspace_bytes", "hag_clip_gradients",
-    "hag_rms_norm", "hag_rms_norm_fp8", "hag_rms_norm_grad_workspace_bytes", "hag_rms_norm_grad", "hag_fp8_product_workspace_bytes", "hag_fp8_product", "hag_adamw",
+    "hag_rms_norm", "hag_rms_norm_fp8", "hag_rms_norm_grad_workspace_bytes", "hag_rms_norm_grad", "hag_fp8_product", "hag_adamw",
 ]
 ROUTES = ("hag", "lists", "component_hag", "component_lists", "dense", "one_launch", "scatter")   # HAG_ROUTE_*
 HAG_STATIC_SCRATCH_BYTES = 64 << 20
@@ -152,9 +152,7 @@ def lib():
         L.hag_rms_norm_grad_workspace_bytes.argtypes = [i64, i64]
         L.hag_rms_norm_grad_workspace_bytes.restype = size_t
         L.hag_rms_norm_grad.argtypes = [i64, i64, i32, vp, i64, vp, i64, vp, i64, i32] + [vp] * 6
-        L.hag_fp8_product_workspace_bytes.argtypes = [i64, i64, i64]
-        L.hag_fp8_product_workspace_bytes.restype = size_t
-        L.hag_fp8_product.argtypes = [i64, i64, i64] + [vp, i64] * 4 + [i32] + [vp] * 3
+        L.hag_fp8_product.argtypes = [i64, i64, i64] + [vp, i64] * 4 + [i32] + [vp] * 2
         L.hag_adamw.argtypes = [i64, vp, ctypes.POINTER(hag_adamw_options_t), vp]
         _lib = L
     return _lib
@@ -784,11 +782,9 @@ def fp8_product(x, x_scales, w, w_scales, dtype=None):
     (n, d), k = x.shape, w.shape[0]
     if w.shape[1] != d:
         raise ValueError(f"x {tuple(x.shape)} and w {tuple(w.shape)} do not match")
-    L = lib()
-    y, nbytes = x.new_empty((n, k), dtype=dtype), L.hag_fp8_product_workspace_bytes(n, d, k)
-    ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-    rc = L.hag_fp8_product(n, d, k, x.data_ptr(), x_strides[0], x_scales.data_ptr(), x_strides[1], w.data_ptr(), w_strides[0], w_scales.data_ptr(), w_strides[1], code, y.data_ptr(),
-                           ws.data_ptr() if nbytes else None, _raw_stream())
+    y = x.new_empty((n, k), dtype=dtype)
+    rc = lib().hag_fp8_product(n, d, k, x.data_ptr(), x_strides[0], x_scales.data_ptr(), x_strides[1], w.data_ptr(), w_strides[0], w_scales.data_ptr(), w_strides[1], code, y.data_ptr(),
+                               _raw_stream())
     if rc != 0:
         _check(rc)
     return y

@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(Produc
     }
 }
 
-// ------------------------------------------------------------------------------------------------ anything else
+// ------------------------------------------------------------------------------------------------ few rows, or rows at any address
 
 // 16 columns from `col` of a row at any address, zeros from column d on
 __device__ __forceinline__ bytes16_t load16(const uint8_t *row, int col, int d) {
@@ -254,30 +254,103 @@ __device__ __forceinline__ bytes16_t load16(const uint8_t *row, int col, int d) 
     }
     return v;
 }
+// What a lane brings of 128 columns from `col` of a row, as it comes from memory
 template <bool WIDE>
-__device__ __forceinline__ Part<WIDE> load_part(const uint8_t *row, const uint8_t *scales, int col, int q, int d) {
-    const int block = col / kScaleBlock;
-    const uint32_t s = WIDE ? load_scale(scales, block + q / 2, d) | load_scale(scales, block + 2 + q / 2, d) << 8 : load_scale(scales, block + q, d);
-    return Part<WIDE>(load16(row, col + 16 * q, d), load16(row, col + 64 + 16 * q, d), s);
+struct Raw {
+    bytes16_t a, b;
+    uint32_t scales;
+    __device__ __forceinline__ void load(const uint8_t *row, const uint8_t *of, int col, int q, int d) {
+        const int block = col / kScaleBlock;
+        a = load16(row, col + 16 * q, d);
+        b = load16(row, col + 64 + 16 * q, d);
+        scales = WIDE ? load_scale(of, block + q / 2, d) | load_scale(of, block + 2 + q / 2, d) << 8 : load_scale(of, block + q, d);
+    }
+    __device__ __forceinline__ operator Part<WIDE>() const { return Part<WIDE>(a, b, scales); }
+};
+
+// A workgroup takes 16 * R rows of x and 32 of w, its wavefronts every so many 128 columns of them, straight from memory; their sums are added up in LDS in their order.
+template <typename O, int R>
+__global__ __launch_bounds__(R == 1 ? 1024 : 512) void product_split_kernel(ProductArgs a) {
+    constexpr bool WIDE = sizeof(O) == 4;
+    __shared__ float4 sums[(R == 1 ? 16 : 8) * R * 2 * kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave, r = lane % 16, q = lane / 16;
+    const int64_t row0 = (int64_t)blockIdx.x * (16 * R), col0 = (int64_t)blockIdx.y * 32;
+    const uint8_t *x[R], *x_scales[R], *w[2], *w_scales[2];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int64_t row = min(row0 + i * 16 + r, a.n - 1);
+        x[i] = a.x + row * a.x_stride;
+        x_scales[i] = a.x_scales + row * a.x_scales_stride;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int64_t row = min(col0 + piece_column<O>(t, r), a.k - 1);
+        w[t] = a.w + row * a.w_stride;
+        w_scales[t] = a.w_scales + row * a.w_scales_stride;
+    }
+    sums_t acc[R][2];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) acc[i][t] = sums_t{0.f, 0.f, 0.f, 0.f};
+    Raw<WIDE> rx[R], rw[2];
+    auto load = [&](int col) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) rw[t].load(w[t], w_scales[t], col, q, a.d);
+#pragma unroll
+        for (int i = 0; i < R; ++i) rx[i].load(x[i], x_scales[i], col, q, a.d);
+    };
+    int col = wave * 128;
+    if (col < a.d) load(col);
+    while (col < a.d) {
+        Raw<WIDE> nx[R], nw[2];
+#pragma unroll
+        for (int i = 0; i < R; ++i) nx[i] = rx[i];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) nw[t] = rw[t];
+        col += waves * 128;
+        if (col < a.d) load(col);                          // the next ones are on their way while these are multiplied
+        const Part<WIDE> pw[2] = {nw[0], nw[1]};
+#pragma unroll
+        for (int i = 0; i < R; ++i) multiply<2>(pw, nx[i], acc[i]);
+    }
+    if (waves > 1) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) sums[((wave * R + i) * 2 + t) * kWave + lane] = make_float4(acc[i][t][0], acc[i][t][1], acc[i][t][2], acc[i][t][3]);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if (i % waves != wave) continue;
+        if (waves > 1) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                acc[i][t] = sums_t{0.f, 0.f, 0.f, 0.f};
+                for (int v = 0; v < waves; ++v) {
+                    const float4 p = sums[((v * R + i) * 2 + t) * kWave + lane];
+                    acc[i][t] += sums_t{p.x, p.y, p.z, p.w};
+                }
+            }
+        }
+        const int64_t row = row0 + i * 16 + r;
+        if (row < a.n) store_columns<O, 2>((O *)a.y + row * a.k + col0, q, (int)min(a.k - col0, (int64_t)32), acc[i]);
+    }
 }
 
-// A wavefront takes 16 rows of x and 64 of w.
-template <typename O>
-__global__ __launch_bounds__(kBlock) void product_kernel(ProductArgs a) {
-    constexpr bool WIDE = sizeof(O) == 4;
-    const int lane = threadIdx.x % kWave, r = lane % 16, q = lane / 16;
-    const int64_t row = ((int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave) * 16 + r, col0 = (int64_t)blockIdx.y * 64, x_row = min(row, a.n - 1);
-    sums_t acc[4] = {};
-    for (int c = 0; c < a.d; c += 128) {
-        Part<WIDE> w[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int64_t w_row = min(col0 + piece_column<O>(t, r), a.k - 1);
-            w[t] = load_part<WIDE>(a.w + w_row * a.w_stride, a.w_scales + w_row * a.w_scales_stride, c, q, a.d);
-        }
-        multiply<4>(w, load_part<WIDE>(a.x + x_row * a.x_stride, a.x_scales + x_row * a.x_scales_stride, c, q, a.d), acc);
-    }
-    if (row < a.n) store_columns<O, 4>((O *)a.y + row * a.k + col0, q, (int)min(a.k - col0, (int64_t)64), acc);
+template <typename O, int R>
+static int launch_split(const ProductArgs &a, hipStream_t s) {
+    const int64_t groups = (a.k + 31) / 32;
+    const unsigned waves = (unsigned)std::min<int64_t>(R == 1 ? 16 : 8, (a.d + 127) / 128);
+    return launch_parts((a.n + 16 * R - 1) / (16 * R), kWave * waves, [&](int64_t first, int64_t count) {
+        ProductArgs part = a;
+        part.x += first * (16 * R) * a.x_stride;
+        part.x_scales += first * (16 * R) * a.x_scales_stride;
+        part.y = (O *)a.y + first * (16 * R) * a.k;
+        part.n = std::min(count * (16 * R), a.n - first * (16 * R));
+        hipLaunchKernelGGL((product_split_kernel<O, R>), dim3((unsigned)count, (unsigned)groups), dim3(kWave * waves), 0, s, part);
+    });
 }
 
 template <typename O, int TM, int TN, int WR, int WC>
@@ -302,10 +375,8 @@ using namespace hag;
 
 extern "C" {
 
-size_t hag_fp8_product_workspace_bytes(int64_t n, int64_t d, int64_t k) { return 0; }
-
 int hag_fp8_product(int64_t n, int64_t d, int64_t k, const uint8_t *x, int64_t x_stride, const uint8_t *x_scales, int64_t x_scales_stride, const uint8_t *w, int64_t w_stride,
-                    const uint8_t *w_scales, int64_t w_scales_stride, hag_dtype_t dtype, void *y, void *workspace, void *stream) {
+                    const uint8_t *w_scales, int64_t w_scales_stride, hag_dtype_t dtype, void *y, void *stream) {
     if (n < 0 || n > 0x7fffffffLL || k < 0 || k > (1 << 20) || d <= 0 || d > (1 << 20)) { set_error("n must be in 0 .. 2^31 - 1, k in 0 .. 2^20, d in 1 .. 2^20"); return HAG_EINVAL; }
     if (!elem_type(dtype)) { set_error("the result is HAG_F32, HAG_BF16 or HAG_F16"); return HAG_EINVAL; }
     if (x_stride < 0 || w_stride < 0 || x_scales_stride < 0 || w_scales_stride < 0) { set_error("negative row stride"); return HAG_EINVAL; }
@@ -317,15 +388,16 @@ int hag_fp8_product(int64_t n, int64_t d, int64_t k, const uint8_t *x, int64_t x
     return elem_switch(dtype, [&](auto e) {
         using O = decltype(e);
         hipStream_t s = (hipStream_t)stream;
-        if (aligned && n > 64) return n * k >= (int64_t)1 << 24 && k > 128 ? (sizeof(O) == 2 ? launch_tiles<O, 256, sizeof(O) == 2 ? 256 : 128, sizeof(O) == 2 ? 2 : 4, sizeof(O) == 2 ? 4 : 2>(a, s) : launch_tiles<O, 256, 128, 4, 2>(a, s)) : launch_tiles<O, 128, 128, 2, 2>(a, s);
-        return launch_parts((n + 63) / 64, kBlock, [&](int64_t first, int64_t count) {
-            ProductArgs part = a;
-            part.x += first * 64 * x_stride;
-            part.x_scales += first * 64 * x_scales_stride;
-            part.y = (O *)a.y + first * 64 * k;
-            part.n = std::min(count * 64, n - first * 64);
-            hipLaunchKernelGGL(product_kernel<O>, dim3((unsigned)count, (unsigned)((k + 63) / 64)), dim3(kBlock), 0, s, part);
-        });
+        // Few workgroups: as small as they come.  64 x 2048 x 2048 into bf16: 16 rows of x each 6.8 us, 32 7.8, 64 10.8 (1 x 512 x 512 3.3, 1 x 2048 x 2048 5.5).  Up to some bytes to read
+        // again they still beat tiles, which wait for memory once per 128 columns: 3000 x 2048 x 64 16 rows 10.9, 32 7.9, 64 10.8, tiles 13.6; 2000 x 256 x 256 4.2, 3.8, 3.9, 4.6;
+        // 1000 x 2048 x 300 15.8, 13.1, 11.1, 14.0; but 2048 x 512 x 512 10.5, 7.9, 6.9, 6.2 and 300 x 2048 x 2048 25.9, 19.3, 20.8, 14.4.
+        const int64_t groups = (k + 31) / 32, tiles = ((n + 127) / 128) * ((k + 127) / 128);
+        if ((n + 15) / 16 * groups <= 256) return launch_split<O, 1>(a, s);
+        if ((n + 31) / 32 * groups * d <= 400000) return launch_split<O, 2>(a, s);
+        if (!aligned || tiles <= 24) return launch_split<O, 4>(a, s);
+        if (n * k < (int64_t)1 << 24 || k <= 128) return launch_tiles<O, 128, 128, 2, 2>(a, s);
+        if constexpr (sizeof(O) == 2) return launch_tiles<O, 256, 256, 2, 4>(a, s);
+        else return launch_tiles<O, 256, 128, 4, 2>(a, s);
     });
 }
 

@@ -47,13 +47,12 @@ def test_product_refusals():
     L = B.lib()
 
     def call(n=2, d=40, k=3, x=P, xs=40, sx=P, ssx=2, w=P, ws=40, sw=P, ssw=2, dtype=0, y=P):
-        return L.hag_fp8_product(n, d, k, x, xs, sx, ssx, w, ws, sw, ssw, dtype, y, P, None)
+        return L.hag_fp8_product(n, d, k, x, xs, sx, ssx, w, ws, sw, ssw, dtype, y, None)
 
     for bad in (dict(n=-1), dict(n=BIG), dict(k=-1), dict(k=(1 << 20) + 1), dict(d=0), dict(d=(1 << 20) + 1), dict(xs=-40), dict(ssx=-1), dict(ws=-1), dict(ssw=-2), dict(dtype=1), dict(dtype=4),
                 dict(x=None), dict(sx=None), dict(w=None), dict(sw=None), dict(y=None)):
         refused(call(**bad))
     assert call(n=0, x=None, sx=None, y=None) == B.HAG_OK and call(k=0, w=None, sw=None, y=None) == B.HAG_OK
-    assert L.hag_fp8_product_workspace_bytes(-1, 4, 4) == 0
 
 
 def test_adamw_refusals():
