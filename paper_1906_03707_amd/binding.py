@@ -810,6 +810,25 @@ def _scalar_at(name, t, dtype, device):
     return t.data_ptr()
 
 
+def _adamw_check(p, g, states, scales, copy, device):
+    """Raises what is wrong with one tensor of adamw and what belongs to it."""
+    import torch
+    codes, whole, count = _elements, p.is_contiguous(), p.numel()
+    if p.dtype not in codes or p.get_device() != device or not (whole or _dense(p)):
+        raise ValueError(f"dense float32, bfloat16 or float16 parameters on the current device are needed, got {p.dtype} {tuple(p.shape)} with strides {tuple(p.stride())} on {p.device}")
+    if g.dtype not in codes or (g.dtype != p.dtype and p.dtype != torch.float32) or g.shape != p.shape or g.get_device() != device or not (whole and g.is_contiguous() or g.stride() == p.stride()):
+        raise ValueError(f"a gradient must match its parameter: {p.dtype} {tuple(p.shape)} with strides {tuple(p.stride())}, got {g.dtype} {tuple(g.shape)} with {tuple(g.stride())}")
+    state_dtype = torch.float8_e4m3fn if scales else torch.float32
+    for t in states:
+        if t.dtype != state_dtype or t.numel() != count or t.get_device() != device or not (t.is_contiguous() or t.shape == p.shape and t.stride() == p.stride()):
+            raise ValueError(f"a state must be {state_dtype}, dense, of its parameter's {count} elements, on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    for t in scales:
+        if t.dtype != torch.float8_e8m0fnu or t.numel() != (count + 31) // 32 or t.get_device() != device or not t.is_contiguous():
+            raise ValueError(f"scales must be contiguous float8_e8m0fnu, {(count + 31) // 32} of them, on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if copy is not None and (copy.dtype not in codes or copy.shape != p.shape or copy.get_device() != device or not (whole and copy.is_contiguous() or copy.stride() == p.stride())):
+        raise ValueError(f"a copy must match its parameter {tuple(p.shape)} with strides {tuple(p.stride())}, got {copy.dtype} {tuple(copy.shape)} with {tuple(copy.stride())}")
+
+
 def adamw(params, grads, m, v, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, norm=None, max_norm=None, copies=None, m_scales=None, v_scales=None, seed=0):
     """One step of AdamW on the tensors `params`, in place, with their gradients and states, lists of one tensor each (hag_adamw).
 
@@ -818,11 +837,14 @@ def adamw(params, grads, m, v, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weig
     device, as clip_gradients returns it) the gradients count as if scaled down to max_norm where it is above, and nothing changes where it is no finite number.  copies: tensors (or
     None) of any of the three types that get the new parameters too.  seed: of the rounding of 8-bit states."""
     import torch
-    device, codes = _device(), _elements or _element_codes()
+    device = _device()
+    _elements or _element_codes()
     bits = 32 if m_scales is None else 8
     params, grads = list(params), list(grads)
-    lists = [list(x) for x in ((m, v) if bits == 32 else (m, v, m_scales, v_scales if v_scales is not None else ()))]
-    if any(len(x) != len(params) for x in (grads, *lists)) or (copies is not None and len(copies) != len(params)) or (m_scales is None and v_scales is not None):
+    m, v = list(m), list(v)
+    copies = [None] * len(params) if copies is None else list(copies)
+    scales = [()] * len(params) if bits == 32 else list(zip(m_scales, v_scales or ()))
+    if not len(params) == len(grads) == len(m) == len(v) == len(scales) == len(copies) or (bits == 32 and v_scales is not None):
         raise ValueError(f"{len(params)} parameters need as many gradients, states, scales of 8-bit states and copies")
     options = hag_adamw_options_t(0.0, betas[0], betas[1], eps, weight_decay, 1.0, 0, None, None, None, seed & 0xFFFFFFFF, bits)
     if isinstance(step, torch.Tensor):
@@ -837,36 +859,25 @@ def adamw(params, grads, m, v, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weig
         raise ValueError("norm and max_norm go together")
     if norm is not None:
         options.norm, options.max_norm = _scalar_at("norm", norm, torch.float32, device), max_norm
-    state_dtype = torch.float32 if bits == 32 else torch.float8_e4m3fn
-    entries, written = [], []
-    for i, (p, g) in enumerate(zip(params, grads)):
-        code, g_code, whole, count = codes.get(p.dtype), codes.get(g.dtype), p.is_contiguous(), p.numel()
-        if code is None or p.get_device() != device or not (whole or _dense(p)):
-            raise ValueError(f"dense float32, bfloat16 or float16 parameters on the current device are needed, got {p.dtype} {tuple(p.shape)} with strides {tuple(p.stride())} on {p.device}")
-        if g_code is None or (g_code != code and code != HAG_F32) or g.shape != p.shape or g.get_device() != device or not (whole and g.is_contiguous() or g.stride() == p.stride()):
-            raise ValueError(f"a gradient must match its parameter: {p.dtype} {tuple(p.shape)} with strides {tuple(p.stride())}, got {g.dtype} {tuple(g.shape)} with {tuple(g.stride())}")
-        at = [p.data_ptr(), g.data_ptr()]
-        for x in lists[:2]:
-            t = x[i]
-            if t.dtype != state_dtype or t.numel() != count or t.get_device() != device or not (t.is_contiguous() or t.shape == p.shape and t.stride() == p.stride()):
-                raise ValueError(f"a state must be {state_dtype}, dense, of its parameter's {count} elements, on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
-            at.append(t.data_ptr())
-        copy, copy_code = copies[i] if copies is not None else None, 0
-        if copy is not None:
-            copy_code = codes.get(copy.dtype)
-            if copy_code is None or copy.shape != p.shape or copy.get_device() != device or not (whole and copy.is_contiguous() or copy.stride() == p.stride()):
-                raise ValueError(f"a copy must match its parameter {tuple(p.shape)} with strides {tuple(p.stride())}, got {copy.dtype} {tuple(copy.shape)} with {tuple(copy.stride())}")
-        at.append(0 if copy is None else copy.data_ptr())
-        for x in lists[2:]:
-            t = x[i]
-            if t.dtype != torch.float8_e8m0fnu or t.numel() != (count + 31) // 32 or t.get_device() != device or not t.is_contiguous():
-                raise ValueError(f"scales must be contiguous float8_e8m0fnu, {(count + 31) // 32} of them, on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
-            at.append(t.data_ptr())
-        if bits == 32:
-            at += (0, 0)
+    codes, state_dtype, entries, written = _elements, torch.float32 if bits == 32 else torch.float8_e4m3fn, [], []
+    for p, g, a, b, sc, copy in zip(params, grads, m, v, scales, copies):
+        code, g_code, count = codes.get(p.dtype), codes.get(g.dtype), p.numel()
+        # tensors of the ordinary kind pass at once, others are looked at one by one
+        if not (code is not None and g_code is not None and (code == g_code or code == HAG_F32) and p.get_device() == g.get_device() == a.get_device() == b.get_device() == device
+                and p.is_contiguous() and g.is_contiguous() and a.is_contiguous() and b.is_contiguous() and a.dtype == b.dtype == state_dtype and a.numel() == b.numel() == count and p.shape == g.shape
+                and (copy is None or copy.dtype in codes and copy.get_device() == device and copy.is_contiguous() and copy.shape == p.shape)
+                and (not sc or sc[0].get_device() == sc[1].get_device() == device and sc[0].is_contiguous() and sc[1].is_contiguous() and sc[0].dtype == sc[1].dtype == torch.float8_e8m0fnu
+                     and sc[0].numel() == sc[1].numel() == (count + 31) // 32)):
+            _adamw_check(p, g, (a, b), sc, copy, device)
         if count:
-            written += [x for x in (at[0], *at[2:]) if x]
-            entries += (*at, count, code | g_code << 32, copy_code)
+            at_p, at_a, at_b, at_copy = p.data_ptr(), a.data_ptr(), b.data_ptr(), 0 if copy is None else copy.data_ptr()
+            at_sa, at_sb = (sc[0].data_ptr(), sc[1].data_ptr()) if sc else (0, 0)
+            entries += (at_p, g.data_ptr(), at_a, at_b, at_copy, at_sa, at_sb, count, code | g_code << 32, 0 if copy is None else codes[copy.dtype])
+            written += (at_p, at_a, at_b)
+            if at_copy:
+                written.append(at_copy)
+            if sc:
+                written += (at_sa, at_sb)
     if len(set(written)) != len(written):
         raise ValueError("a tensor is named twice")
     table = array.array("q", entries)
