@@ -50,7 +50,8 @@ __device__ __forceinline__ double power(double b, int64_t t) {
 }
 
 struct AdamNumbers {
-    double clip;
+    float clip, clip_rest;                                 // the factor is (clip + clip_rest) * 2^clip_exponent, clip in [1/2, 1]: their products with a gradient are rounded once
+    int clip_exponent;
     float b1, a1, b2, a2, keep, rate, root, eps;           // a: 1 - b;  keep: 1 - lr decay, rate: lr / (1 - b1^t), root: 1 / sqrt(1 - b2^t)
     uint32_t key;
 };
@@ -114,97 +115,152 @@ __device__ __forceinline__ void decode4(uint32_t codes, uint32_t byte, float (&v
     v[3] = b.y * scale;
 }
 
-// An element in 8 bits, rounded up where its 16 random bits and the part that is cut off, in 2^-16 of a step, and a half make more than a step.  |v| / scale as a float of an exponent
-// bias of 7 instead of 127 is |v| / scale * 2^-120, whose upper bits then are the element's.
-__device__ __forceinline__ uint32_t dithered(float v, uint32_t byte, uint32_t random, bool keep) {
-    const uint32_t bits = __float_as_uint(ldexpf(fabsf(v), 7 - (int)byte));       // 127 - byte - 120
-    uint32_t code = (bits + (random << 4) + 8u) >> 20;
-    if (keep && v != 0.f) code = max(code, 1u);
-    if (!(fabsf(v) < INFINITY)) code = 0x7fu;
-    return code | (__float_as_uint(v) >> 31 << 7);
+// The amount of an element in 8 bits, rounded up where its 16 random bits (`random`, 16 times as much) and the part that is cut off, in 2^-16 of a step, and a half make more than a step.
+// |v| / scale as a float of an exponent bias of 7 instead of 127 is |v| / scale * 2^-120, whose upper bits then are the element's.
+__device__ __forceinline__ uint32_t dithered(float v, uint32_t byte, uint32_t random) {
+    return (__float_as_uint(ldexpf(fabsf(v), 7 - (int)byte)) + random + 8u) >> 20;         // 127 - byte - 120
 }
 
-// Four elements of a tensor, `have` of them there; element: the number of the first.  Eight adjacent lanes have a block's.
-template <typename P, typename G, int BITS>
-__device__ __forceinline__ void adam4(const AdamArgs::Tensor &t, const AdamNumbers &a, int64_t element, int have) {
+// Four elements of a tensor, `have` of them there (FULL: all), as they come from memory.  Eight adjacent lanes have a block's.
+template <typename P, typename G, int BITS, bool FULL>
+struct AdamFour {
+    int64_t element;                 // the number of the first
+    int have;
+    typename Four<P>::type p;
+    typename Four<G>::type g;
+    typename Four<float>::type m, v;
+    uint32_t m_codes, v_codes, m_byte, v_byte;
+
+    __device__ __forceinline__ void load(const AdamArgs::Tensor &t, int64_t first, int there) {
+        element = first;
+        have = FULL ? 4 : there;
+        p = load4((const P *)t.param + element, have);
+        g = load4((const G *)t.grad + element, have);
+        if (BITS == 32) {
+            m = load4((const float *)t.m + element, have);
+            v = load4((const float *)t.v + element, have);
+            return;
+        }
+        const bool in = have > 0;
+        m_codes = load_codes((const uint8_t *)t.m + element, have);
+        v_codes = load_codes((const uint8_t *)t.v + element, have);
+        m_byte = in ? t.m_scales[element / kScaleBlock] : 127u;
+        v_byte = in ? t.v_scales[element / kScaleBlock] : 127u;
+    }
+
+    __device__ __forceinline__ void step(const AdamArgs::Tensor &t, const AdamNumbers &a) {
 // what the 8-bit states are rounded from is the same everywhere, whatever is fused: products and sums are rounded one by one
 #pragma clang fp contract(off)
-    const typename Four<P>::type praw = load4((const P *)t.param + element, have);
-    const typename Four<G>::type graw = load4((const G *)t.grad + element, have);
-    float m[4], root[4], v[4];
-    if (BITS == 8) {
-        const bool in = have > 0;
-        decode4(load_codes((const uint8_t *)t.m + element, have), in ? t.m_scales[element / kScaleBlock] : 127u, m);
-        decode4(load_codes((const uint8_t *)t.v + element, have), in ? t.v_scales[element / kScaleBlock] : 127u, v);
-    } else {
-        const typename Four<float>::type mraw = load4((const float *)t.m + element, have), vraw = load4((const float *)t.v + element, have);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { m[e] = mraw[e]; v[e] = vraw[e]; }
-    }
-    float p[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float g = (float)((double)(float)graw[e] * a.clip);
-        m[e] = a.b1 * m[e] + a.a1 * g;
+        float nm[4], nv[4], np[4];
         if (BITS == 8) {
-            root[e] = v[e] = sqrtf(a.b2 * (v[e] * v[e]) + a.a2 * (g * g));
-        } else {
-            v[e] = a.b2 * v[e] + a.a2 * (g * g);
-            root[e] = sqrtf(v[e]);
+            decode4(m_codes, m_byte, nm);
+            decode4(v_codes, v_byte, nv);
         }
-        p[e] = (float)praw[e] * a.keep - a.rate * (m[e] / (root[e] * a.root + a.eps));
-    }
-    store4((P *)t.param + element, have, p);
-    const int copy = t.types >> 16 & 0xff;
-    if (t.copy) {
-        if (copy == HAG_BF16) store4((bf16_t *)t.copy + element, have, p);
-        else if (copy == HAG_F16) store4((f16_t *)t.copy + element, have, p);
-        else store4((float *)t.copy + element, have, p);
-    }
-    if (BITS == 32) {
-        store4((float *)t.m + element, have, m);
-        store4((float *)t.v + element, have, v);
-        return;
-    }
-    float most_m = 0.f, most_v = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        most_m = fmaxf(most_m, e < have ? finite_amount(m[e]) : 0.f);
-        most_v = fmaxf(most_v, e < have ? finite_amount(v[e]) : 0.f);
-    }
-    const uint32_t byte_m = scale_byte(lanes_max<8>(most_m)), byte_v = scale_byte(lanes_max<8>(most_v));
-    uint32_t codes_m = 0, codes_v = 0;
+        for (int e = 0; e < 4; ++e) {
+            const float d = ldexpf(fmaf((float)g[e], a.clip, (float)g[e] * a.clip_rest), a.clip_exponent);
+            nm[e] = a.b1 * (BITS == 8 ? nm[e] : m[e]) + a.a1 * d;
+            float root;
+            if (BITS == 8) {
+                root = nv[e] = sqrtf(a.b2 * (nv[e] * nv[e]) + a.a2 * (d * d));
+            } else {
+                nv[e] = a.b2 * v[e] + a.a2 * (d * d);
+                root = __builtin_amdgcn_sqrtf(nv[e]);      // (one unit in the last place, as the reciprocal)
+            }
+            np[e] = (float)p[e] * a.keep - a.rate * (nm[e] * __builtin_amdgcn_rcpf(root * a.root + a.eps));
+        }
+        store4((P *)t.param + element, have, np);
+        if (t.copy) {
+            const int copy = t.types >> 16 & 0xff;
+            if (copy == HAG_BF16) store4((bf16_t *)t.copy + element, have, np);
+            else if (copy == HAG_F16) store4((f16_t *)t.copy + element, have, np);
+            else store4((float *)t.copy + element, have, np);
+        }
+        if (BITS == 32) {
+            store4((float *)t.m + element, have, nm);
+            store4((float *)t.v + element, have, nv);
+            return;
+        }
+        // the largest amounts, and whether all are numbers: as whole numbers, those that are none are above all others
+        uint32_t most_m = 0, most_v = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const uint64_t at = (uint64_t)element + e;
-        const uint32_t random = mixed((uint32_t)at * 0x9e3779b1u + a.key + (uint32_t)(at >> 32) * 0x85ebca6bu);
-        codes_m |= dithered(m[e], byte_m, random & 0xffffu, false) << 8 * e;
-        codes_v |= dithered(v[e], byte_v, random >> 16, true) << 8 * e;
+        for (int e = 0; e < 4; ++e) {
+            if (!FULL && e >= have) nm[e] = nv[e] = 0.f;
+            most_m = max(most_m, __float_as_uint(nm[e]) & 0x7fffffffu);
+            most_v = max(most_v, __float_as_uint(nv[e]) & 0x7fffffffu);
+        }
+        const bool numbers = max(most_m, most_v) < 0x7f800000u;
+        uint32_t none = 0;                                 // bits of m's and v's elements that are none
+        if (__any(!numbers)) {
+            most_m = most_v = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!(fabsf(nm[e]) < INFINITY)) { none |= 1u << e; nm[e] = 0.f; }
+                if (!(fabsf(nv[e]) < INFINITY)) { none |= 16u << e; nv[e] = 0.f; }
+                most_m = max(most_m, __float_as_uint(nm[e]) & 0x7fffffffu);
+                most_v = max(most_v, __float_as_uint(nv[e]) & 0x7fffffffu);
+            }
+        }
+        const uint32_t byte_m = scale_byte(lanes_max<8>(__uint_as_float(most_m))), byte_v = scale_byte(lanes_max<8>(__uint_as_float(most_v)));
+        uint32_t codes_m = 0, codes_v = 0;
+        const uint32_t place = (uint32_t)element * 0x9e3779b1u + a.key + (uint32_t)(element >> 32) * 0x85ebca6bu;   // (four elements do not cross 2^32)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t random = mixed(place + (uint32_t)e * 0x9e3779b1u);
+            codes_m |= (dithered(nm[e], byte_m, random << 4 & 0xffff0u) | (__float_as_uint(nm[e]) >> 24 & 0x80u)) << 8 * e;
+            codes_v |= max(dithered(nv[e], byte_v, random >> 12 & 0xffff0u), nv[e] != 0.f ? 1u : 0u) << 8 * e;
+        }
+        if (__any(none)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (none >> e & 1) codes_m |= 0x7fu << 8 * e;
+                if (none >> e & 16) codes_v |= 0x7fu << 8 * e;
+            }
+        }
+        store_codes((uint8_t *)t.m + element, have, codes_m);
+        store_codes((uint8_t *)t.v + element, have, codes_v);
+        if (have > 0 && threadIdx.x % 8 == 0) {
+            t.m_scales[element / kScaleBlock] = (uint8_t)byte_m;
+            t.v_scales[element / kScaleBlock] = (uint8_t)byte_v;
+        }
     }
-    store_codes((uint8_t *)t.m + element, have, codes_m);
-    store_codes((uint8_t *)t.v + element, have, codes_v);
-    if (have > 0 && threadIdx.x % 8 == 0) {
-        t.m_scales[element / kScaleBlock] = (uint8_t)byte_m;
-        t.v_scales[element / kScaleBlock] = (uint8_t)byte_v;
-    }
-}
+};
 
+// Pieces that a workgroup requests one after the other before it needs the first
+constexpr int kAdamAsk = 2;
 template <typename P, typename G, int BITS>
 __device__ __forceinline__ void adam_unit(const AdamArgs::Tensor &t, const AdamNumbers &a, int64_t begin, int64_t end) {
-    for (int64_t at = begin; at < end; at += 4 * kBlock) {
-        const int64_t element = at + 4 * (int)threadIdx.x;
-        adam4<P, G, BITS>(t, a, element, (int)max((int64_t)0, min(end - element, (int64_t)4)));
+    constexpr int kPiece = 4 * kBlock;
+    const int mine = 4 * (int)threadIdx.x;
+    int64_t at = begin;
+    for (; at + kAdamAsk * kPiece <= end; at += kAdamAsk * kPiece) {
+        AdamFour<P, G, BITS, true> f[kAdamAsk];
+#pragma unroll
+        for (int u = 0; u < kAdamAsk; ++u) f[u].load(t, at + u * kPiece + mine, 4);
+#pragma unroll
+        for (int u = 0; u < kAdamAsk; ++u) f[u].step(t, a);
+    }
+    for (; at < end; at += kPiece) {
+        AdamFour<P, G, BITS, false> f;
+        f.load(t, at + mine, (int)max((int64_t)0, min(end - at - mine, (int64_t)4)));
+        f.step(t, a);
     }
 }
 
 template <int BITS>
 __global__ __launch_bounds__(kBlock) void adamw_kernel(AdamArgs a) {
     AdamNumbers s;
-    s.clip = 1.;
+    s.clip = 1.f;
+    s.clip_rest = 0.f;
+    s.clip_exponent = 0;
     if (a.norm) {
         const float norm = *a.norm;
         if (!(fabsf(norm) < INFINITY)) return;             // nothing changes
-        if (norm > a.max_norm) s.clip = a.max_norm / norm;
+        if (norm > a.max_norm) {
+            const double factor = frexp(a.max_norm / norm, &s.clip_exponent);
+            s.clip = (float)factor;
+            s.clip_rest = (float)(factor - s.clip);
+        }
     }
     const double lr = a.lr_at ? (double)*a.lr_at : a.lr;
     const int64_t step = a.step_at ? *a.step_at : a.step;
