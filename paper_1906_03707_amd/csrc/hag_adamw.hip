@@ -115,37 +115,48 @@ __device__ __forceinline__ void decode4(uint32_t codes, uint32_t byte, float (&v
     v[3] = b.y * scale;
 }
 
-// The amount of an element in 8 bits, rounded up where its 16 random bits (`random`, 16 times as much) and the part that is cut off, in 2^-16 of a step, and a half make more than a step.
+// The amount of an element in 8 bits, rounded up where its 16 random bits and a half (`random`, 16 times as much) and the part that is cut off, in 2^-16 of a step, make more than a step.
 // |v| / scale as a float of an exponent bias of 7 instead of 127 is |v| / scale * 2^-120, whose upper bits then are the element's.
 __device__ __forceinline__ uint32_t dithered(float v, uint32_t byte, uint32_t random) {
-    return (__float_as_uint(ldexpf(fabsf(v), 7 - (int)byte)) + random + 8u) >> 20;         // 127 - byte - 120
+    return (__float_as_uint(ldexpf(fabsf(v), 7 - (int)byte)) + random) >> 20;         // 127 - byte - 120
 }
 
-// Four elements of a tensor, `have` of them there (FULL: all), as they come from memory.  Eight adjacent lanes have a block's.
+// The root rounded correctly, as IEEE's: the hardware's is at most one unit off, and the remainders at the numbers beside it say which way.  (Below 2^-100 those lose bits, and it is as
+// good as the hardware's.)
+__device__ __forceinline__ float root_of(float x) {
+    const float s = __builtin_amdgcn_sqrtf(x), down = __uint_as_float(__float_as_uint(s) - 1u), up = __uint_as_float(__float_as_uint(s) + 1u);
+    const float r = fmaf(-down, s, x) <= 0.f ? down : s;   // (of zero, infinity and no number: comparisons with no number, s stays)
+    return fmaf(-up, s, x) > 0.f ? up : r;
+}
+
+// Four elements of a tensor, `have` of them there (FULL: all), as they come from memory: elements at + mine and on, `at` the workgroup's, a multiple of 1024.  Eight adjacent lanes have a
+// block's.
 template <typename P, typename G, int BITS, bool FULL>
 struct AdamFour {
-    int64_t element;                 // the number of the first
+    int64_t at;
+    uint32_t mine;
     int have;
     typename Four<P>::type p;
     typename Four<G>::type g;
     typename Four<float>::type m, v;
     uint32_t m_codes, v_codes, m_byte, v_byte;
 
-    __device__ __forceinline__ void load(const AdamArgs::Tensor &t, int64_t first, int there) {
-        element = first;
+    __device__ __forceinline__ void load(const AdamArgs::Tensor &t, int64_t first, uint32_t lane, int there) {
+        at = first;
+        mine = lane;
         have = FULL ? 4 : there;
-        p = load4((const P *)t.param + element, have);
-        g = load4((const G *)t.grad + element, have);
+        p = load4((const P *)t.param + at + mine, have);
+        g = load4((const G *)t.grad + at + mine, have);
         if (BITS == 32) {
-            m = load4((const float *)t.m + element, have);
-            v = load4((const float *)t.v + element, have);
+            m = load4((const float *)t.m + at + mine, have);
+            v = load4((const float *)t.v + at + mine, have);
             return;
         }
         const bool in = have > 0;
-        m_codes = load_codes((const uint8_t *)t.m + element, have);
-        v_codes = load_codes((const uint8_t *)t.v + element, have);
-        m_byte = in ? t.m_scales[element / kScaleBlock] : 127u;
-        v_byte = in ? t.v_scales[element / kScaleBlock] : 127u;
+        m_codes = load_codes((const uint8_t *)t.m + at + mine, have);
+        v_codes = load_codes((const uint8_t *)t.v + at + mine, have);
+        m_byte = in ? (t.m_scales + at / kScaleBlock)[mine / kScaleBlock] : 127u;
+        v_byte = in ? (t.v_scales + at / kScaleBlock)[mine / kScaleBlock] : 127u;
     }
 
     __device__ __forceinline__ void step(const AdamArgs::Tensor &t, const AdamNumbers &a) {
@@ -162,32 +173,32 @@ struct AdamFour {
             nm[e] = a.b1 * (BITS == 8 ? nm[e] : m[e]) + a.a1 * d;
             float root;
             if (BITS == 8) {
-                root = nv[e] = sqrtf(a.b2 * (nv[e] * nv[e]) + a.a2 * (d * d));
+                root = nv[e] = root_of(a.b2 * (nv[e] * nv[e]) + a.a2 * (d * d));
             } else {
                 nv[e] = a.b2 * v[e] + a.a2 * (d * d);
                 root = __builtin_amdgcn_sqrtf(nv[e]);      // (one unit in the last place, as the reciprocal)
             }
-            np[e] = (float)p[e] * a.keep - a.rate * (nm[e] * __builtin_amdgcn_rcpf(root * a.root + a.eps));
+            np[e] = fmaf(-a.rate, nm[e] * __builtin_amdgcn_rcpf(fmaf(root, a.root, a.eps)), (float)p[e] * a.keep);
         }
-        store4((P *)t.param + element, have, np);
+        store4((P *)t.param + at + mine, have, np);
         if (t.copy) {
             const int copy = t.types >> 16 & 0xff;
-            if (copy == HAG_BF16) store4((bf16_t *)t.copy + element, have, np);
-            else if (copy == HAG_F16) store4((f16_t *)t.copy + element, have, np);
-            else store4((float *)t.copy + element, have, np);
+            if (copy == HAG_BF16) store4((bf16_t *)t.copy + at + mine, have, np);
+            else if (copy == HAG_F16) store4((f16_t *)t.copy + at + mine, have, np);
+            else store4((float *)t.copy + at + mine, have, np);
         }
         if (BITS == 32) {
-            store4((float *)t.m + element, have, nm);
-            store4((float *)t.v + element, have, nv);
+            store4((float *)t.m + at + mine, have, nm);
+            store4((float *)t.v + at + mine, have, nv);
             return;
         }
-        // the largest amounts, and whether all are numbers: as whole numbers, those that are none are above all others
+        // the largest amounts, and whether all are numbers: as whole numbers, those that are none are above all others (roots have no sign)
         uint32_t most_m = 0, most_v = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (!FULL && e >= have) nm[e] = nv[e] = 0.f;
             most_m = max(most_m, __float_as_uint(nm[e]) & 0x7fffffffu);
-            most_v = max(most_v, __float_as_uint(nv[e]) & 0x7fffffffu);
+            most_v = max(most_v, __float_as_uint(nv[e]));
         }
         const bool numbers = max(most_m, most_v) < 0x7f800000u;
         uint32_t none = 0;                                 // bits of m's and v's elements that are none
@@ -203,12 +214,12 @@ struct AdamFour {
         }
         const uint32_t byte_m = scale_byte(lanes_max<8>(__uint_as_float(most_m))), byte_v = scale_byte(lanes_max<8>(__uint_as_float(most_v)));
         uint32_t codes_m = 0, codes_v = 0;
-        const uint32_t place = (uint32_t)element * 0x9e3779b1u + a.key + (uint32_t)(element >> 32) * 0x85ebca6bu;   // (four elements do not cross 2^32)
+        const uint32_t place = ((uint32_t)at + mine) * 0x9e3779b1u + a.key + (uint32_t)(at >> 32) * 0x85ebca6bu;    // (a piece does not cross 2^32)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint32_t random = mixed(place + (uint32_t)e * 0x9e3779b1u);
-            codes_m |= (dithered(nm[e], byte_m, random << 4 & 0xffff0u) | (__float_as_uint(nm[e]) >> 24 & 0x80u)) << 8 * e;
-            codes_v |= max(dithered(nv[e], byte_v, random >> 12 & 0xffff0u), nv[e] != 0.f ? 1u : 0u) << 8 * e;
+            codes_m |= (dithered(nm[e], byte_m, (random << 4 & 0xffff0u) | 8u) | (__float_as_uint(nm[e]) >> 24 & 0x80u)) << 8 * e;
+            codes_v |= max(dithered(nv[e], byte_v, (random >> 12 & 0xffff0u) | 8u), min(__float_as_uint(nv[e]), 1u)) << 8 * e;
         }
         if (__any(none)) {
 #pragma unroll
@@ -217,11 +228,11 @@ struct AdamFour {
                 if (none >> e & 16) codes_v |= 0x7fu << 8 * e;
             }
         }
-        store_codes((uint8_t *)t.m + element, have, codes_m);
-        store_codes((uint8_t *)t.v + element, have, codes_v);
+        store_codes((uint8_t *)t.m + at + mine, have, codes_m);
+        store_codes((uint8_t *)t.v + at + mine, have, codes_v);
         if (have > 0 && threadIdx.x % 8 == 0) {
-            t.m_scales[element / kScaleBlock] = (uint8_t)byte_m;
-            t.v_scales[element / kScaleBlock] = (uint8_t)byte_v;
+            (t.m_scales + at / kScaleBlock)[mine / kScaleBlock] = (uint8_t)byte_m;
+            (t.v_scales + at / kScaleBlock)[mine / kScaleBlock] = (uint8_t)byte_v;
         }
     }
 };
@@ -231,18 +242,18 @@ constexpr int kAdamAsk = 2;
 template <typename P, typename G, int BITS>
 __device__ __forceinline__ void adam_unit(const AdamArgs::Tensor &t, const AdamNumbers &a, int64_t begin, int64_t end) {
     constexpr int kPiece = 4 * kBlock;
-    const int mine = 4 * (int)threadIdx.x;
+    const uint32_t mine = 4 * threadIdx.x;
     int64_t at = begin;
     for (; at + kAdamAsk * kPiece <= end; at += kAdamAsk * kPiece) {
         AdamFour<P, G, BITS, true> f[kAdamAsk];
 #pragma unroll
-        for (int u = 0; u < kAdamAsk; ++u) f[u].load(t, at + u * kPiece + mine, 4);
+        for (int u = 0; u < kAdamAsk; ++u) f[u].load(t, at + u * kPiece, mine, 4);
 #pragma unroll
         for (int u = 0; u < kAdamAsk; ++u) f[u].step(t, a);
     }
     for (; at < end; at += kPiece) {
         AdamFour<P, G, BITS, false> f;
-        f.load(t, at + mine, (int)max((int64_t)0, min(end - at - mine, (int64_t)4)));
+        f.load(t, at, mine, (int)max((int64_t)0, min(end - at - (int64_t)mine, (int64_t)4)));
         f.step(t, a);
     }
 }
