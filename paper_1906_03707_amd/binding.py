@@ -771,7 +771,7 @@ def _rows_fp8(name, codes, scales, device):
 
 
 def fp8_product(x, x_scales, w, w_scales, dtype=None):
-    """x w^T [n, k] of rows in 8 bits, x [n, d] and w [k, d] as rms_norm_fp8 and quantize_fp8 give them; dtype: float32 (the default), bfloat16 or float16 (hag_fp8_product)."""
+    """x w^T [n, k] of rows in 8 bits, x [n, d] and w [k, d] as rms_norm_fp8 and layers.quantize_fp8 give them; dtype: float32 (the default), bfloat16 or float16 (hag_fp8_product)."""
     import torch
     device = _device()
     dtype = torch.float32 if dtype is None else dtype

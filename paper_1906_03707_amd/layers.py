@@ -1,7 +1,7 @@
 """The two GNN layers of the paper's Table 1 around the library's aggregation calls.
 
 The aggregation (and, for GCN, the normalisation fused into it), the gradients of the weight matrices,
-the SoftMax loss, lookups of nodes' rows in a table, layer norm and the clipping of gradients are this library's
+the SoftMax loss, lookups of nodes' rows in a table, layer norm, root-mean-square norm, the clipping of gradients, AdamW and products of 8-bit rows are this library's
 kernels; the other dense parts (products with the weight matrices, ReLU) are plain torch.  Each aggregation call can be recorded (its input and
 output tensors), so that a test can hand exactly those inputs to the CPU oracle.
 
@@ -143,6 +143,45 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
     return _LayerNorm.apply(x, weight, bias, eps)
 
 
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, eps, residual):
+        rows = _rows_of(x)
+        y, h, rstd = binding.rms_norm(rows, weight, eps, None if residual is None else _rows_of(residual))
+        ctx.save_for_backward(h, weight, rstd)
+        ctx.shape = x.shape
+        ctx.set_materialize_grads(False)
+        return y.view(x.shape) if residual is None else (y.view(x.shape), h.view(x.shape))
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g_y, g_h=None):
+        h, weight, rstd = ctx.saved_tensors
+        if g_y is None:                                    # only the sum was used
+            return g_h, None, None, g_h if ctx.needs_input_grad[3] else None
+        g_x, g_w = binding.rms_norm_grad(_rows_of(g_y), h, rstd, weight, None if g_h is None else _rows_of(g_h), params=ctx.needs_input_grad[1])
+        g_x = g_x.view(ctx.shape)
+        return g_x, g_w, None, g_x if ctx.needs_input_grad[3] else None
+
+
+def rms_norm(x, weight=None, eps=1e-5, residual=None):
+    """h / sqrt(mean of h^2 + eps) * weight over the last dimension of h = x + residual (float32, bfloat16 or float16, both alike), weight [d] of that type or float32.  With a residual
+    (y, h): h goes on to the next layer, past what is computed from y.  Its backward pass is not itself differentiable."""
+    return _RmsNorm.apply(x, weight, eps, residual)
+
+
+def quantize_fp8(w):
+    """Rows [k, d] in 8 bits, as rms_norm_fp8 leaves them: (codes, scales), a power of two for every 32 columns, elements to the nearest.  Plain torch: for weights, once."""
+    k, d = w.shape
+    w = w.float()
+    most = torch.nn.functional.pad(w.abs(), (0, -d % 32)).reshape(k, (d + 31) // 32, 32).amax(2)
+    fraction, exponent = torch.frexp(most)
+    e = torch.where(fraction == 0, 0, (exponent - 9 + (fraction > 0.875)).clamp(min=-127))                 # the smallest with most <= 448 * 2^e
+    codes = torch.zeros(k, (d + 15) // 16 * 16, dtype=torch.float8_e4m3fn, device=w.device)
+    codes[:, :d] = torch.ldexp(w, -e.repeat_interleave(32, 1)[:, :d]).to(torch.float8_e4m3fn)
+    return codes[:, :d], (e + 127).to(torch.uint8).view(torch.float8_e8m0fnu)
+
+
 def clip_gradients(parameters, max_norm):
     """Scales the gradients of `parameters` (those that have one) down, in place, so that their 2-norm, taken as one vector, is at most max_norm.  The norm they had, a float32
     scalar on the device: nothing waits for it.  An infinite gradient leaves zeros and NaN, a NaN all NaN, so look at it before the parameters are changed where that can happen."""
@@ -151,6 +190,44 @@ def clip_gradients(parameters, max_norm):
     if grads:
         torch.autograd.graph.increment_version(grads)
     return norm
+
+
+class AdamW:
+    """AdamW (hag_adamw) for float32, bfloat16 or float16 leaves.  bits: of its states, 32 (two float32 numbers for each element) or 8 (two bytes and a sixteenth, rounded by chance from `seed` and
+    the step so that their means are kept).  lr may be changed between steps; one count of steps for all parameters."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, seed=0):
+        self.params, self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.seed, self.steps = list(params), lr, betas, eps, weight_decay, bits, seed, 0
+        self.states = binding.adamw_states(self.params, bits)
+
+    def zero_grad(self):
+        for p in self.params:
+            p.grad = None
+
+    def step(self, max_norm=None):
+        """One step on the parameters that have a gradient.  max_norm: as if their gradients were scaled down to that norm, which they are not; the norm they have, a float32 scalar on
+        the device, is returned (nothing waits for it), and where it is no finite number no parameter and no state changes."""
+        at = [i for i, p in enumerate(self.params) if p.grad is not None]
+        params = [self.params[i] for i in at]
+        grads = [p.grad if p.grad.stride() == p.stride() or p.is_contiguous() and p.grad.is_contiguous() else torch.empty_like(p, dtype=p.grad.dtype).copy_(p.grad) for p in params]
+        norm = None if max_norm is None else binding.clip_gradients(grads, float("inf"))
+        self.steps += 1
+        binding.adamw([p.detach() for p in params], grads, **{k: [x[i] for i in at] for k, x in self.states.items()}, step=self.steps, lr=self.lr, betas=self.betas, eps=self.eps,
+                      weight_decay=self.weight_decay, norm=norm, max_norm=max_norm, seed=self.seed)
+        if params:
+            torch.autograd.graph.increment_version(params)
+        return norm
+
+    def state_dict(self):
+        return {"steps": self.steps, "bits": self.bits, "seed": self.seed, "states": {k: [t.clone() for t in x] for k, x in self.states.items()}}
+
+    def load_state_dict(self, d):
+        if d["bits"] != self.bits or any([t.shape for t in x] != [t.shape for t in d["states"][k]] for k, x in self.states.items()):
+            raise ValueError("states of other parameters or bits")
+        self.steps, self.seed = d["steps"], d["seed"]
+        for k, x in self.states.items():
+            for t, u in zip(x, d["states"][k]):
+                t.view(torch.uint8).copy_(u.view(torch.uint8))
 
 
 def aggregation(h, op, naive=False, record=None):
@@ -263,6 +340,52 @@ def embedded_gcn2_step(h, ids, params, labels, lr, max_norm, padding=None):
         for p in params:
             p.sub_(p.grad, alpha=lr)
     return loss.detach(), norm
+
+
+def residual_gcn_logits(h, ids, params, padding=None, naive=False):
+    """Logits of a GCN of any number of layers around a sum that every layer adds to: x' = x + relu(gcn_agg(norm(x) W)) from a table's rows, then gcn_agg(norm(x) W) with the last matrix, norm
+    being root-mean-square norm.  params: (table, then a norm's weight [d] and a matrix [d, d] for each layer, a last weight [d] and matrix [d, classes])."""
+    table, *rest = params
+    agg = aggregation(h, "gcn", naive)
+    x, update = embedding(table, ids, table.shape[1] ** 0.5, padding), None
+    for k in range(0, len(rest), 2):
+        if update is None:
+            n = rms_norm(x, rest[k])
+        else:
+            n, x = rms_norm(update, rest[k], residual=x)
+        z = agg(product(n, rest[k + 1]))
+        update = torch.relu(z)
+    return z
+
+
+def residual_gcn_step(h, ids, params, labels, optimizer, max_norm=None, padding=None):
+    """One step of an AdamW over `params` on the SoftMax loss of residual_gcn_logits; (loss, gradient norm or None), scalars on the device."""
+    optimizer.zero_grad()
+    loss = softmax_loss(residual_gcn_logits(h, ids, params, padding), labels)
+    loss.backward()
+    return loss.detach(), optimizer.step(max_norm)
+
+
+def residual_gcn_fp8(params):
+    """`params` of residual_gcn_logits for serving: its matrices in 8 bits, one row for each of their columns."""
+    table, *rest = (p.detach() for p in params)
+    return table, [(rest[k], *quantize_fp8(rest[k + 1].t().contiguous())) for k in range(0, len(rest), 2)]
+
+
+def residual_gcn_logits_fp8(h, ids, served, padding=None, naive=False):
+    """residual_gcn_logits (inference) with the rows that the norms leave, and the matrices of residual_gcn_fp8, in 8 bits; sums, aggregation and the residual in float32."""
+    with torch.no_grad():
+        table, layers = served
+        forward = h.naive_forward if naive else h.forward
+        x, update = embedding(table, ids, table.shape[1] ** 0.5, padding).float(), None
+        for weight, codes, scales in layers:
+            if update is None:
+                n, n_scales, _ = binding.rms_norm_fp8(x, weight)
+            else:
+                n, n_scales, x = binding.rms_norm_fp8(update, weight, residual=x)
+            z = forward(binding.fp8_product(n, n_scales, codes, scales), "gcn")
+            update = torch.relu(z)
+        return z
 
 
 def sage_pool2_loss(h, x, pool, comb, labels, naive=False, record=None):

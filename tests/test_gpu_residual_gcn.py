@@ -1,0 +1,252 @@
+"""RMS norm under autograd, AdamW as an optimiser, and the model of many layers that trains and serves with them: against the same model in 64 bits."""
+import math
+import os
+import sys
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1906_03707_amd import binding
+    binding.lib()
+    return binding
+
+
+def near(got, want, tol):
+    return (got.double() - want.double()).norm().item() <= tol * want.double().norm().item()
+
+
+def norm64(x, w, eps=1e-5):
+    return x * (x.square().mean(-1, keepdim=True) + eps).rsqrt() * (1.0 if w is None else w)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_under_autograd(B, dtype):
+    from paper_1906_03707_amd import layers
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, res = (torch.randn(4, 7, 12, device="cuda", generator=gen).to(dtype) for _ in range(2))
+    w = 1 + 0.2 * torch.randn(12, device="cuda", generator=gen)
+    tol = 1e-5 if dtype == torch.float32 else 2e-2
+    scale = torch.arange(7, device="cuda")[:, None]
+
+    def run(norm, cast, uses_h, uses_y=True):
+        a, b, ww = (cast(t).requires_grad_() for t in (x, res, w))
+        y, h = norm(a, ww, b)
+        loss = 0
+        if uses_y:                                         # (gradients that reach the norm are broadcast and transposed ones)
+            loss = y.float().sum() + (y.transpose(0, 2).float() * scale).sum() + (y.float() ** 3).sum()
+        if uses_h:
+            loss = loss + (h.float().transpose(0, 1) ** 2).sum()
+        return y, h, torch.autograd.grad(loss, (a, b, ww) if uses_y else (a, b))
+
+    for uses in ((False, True), (True, True), (True, False)):
+        y, h, grads = run(lambda a, ww, b: layers.rms_norm(a, ww, residual=b), lambda t: t.clone(), *uses)
+        want_y, want_h, want = run(lambda a, ww, b: (norm64(a + b, ww), a + b), lambda t: t.double(), *uses)
+        assert y.shape == h.shape == (4, 7, 12) and y.dtype == h.dtype == dtype
+        assert near(y.detach(), want_y.detach(), tol) and near(h.detach(), want_h.detach(), tol)
+        assert all(near(g, q, 4 * tol) for g, q in zip(grads, want)) and grads[0].shape == x.shape and grads[-1].dtype == (w if uses[1] else x).dtype
+    leaf = x.clone().requires_grad_()
+    layers.rms_norm(leaf[..., :5]).float().square().sum().backward()               # a view, no weight
+    assert leaf.grad.shape == x.shape and not bool(leaf.grad[..., 5:].any())
+    both = x.clone().requires_grad_()
+    y, h = layers.rms_norm(both, residual=both)            # one tensor twice: its gradient counts twice
+    (h.float() * 3).sum().backward()
+    assert bool((both.grad == 6).all())
+    with pytest.raises(RuntimeError):                                              # not twice
+        g, = torch.autograd.grad(layers.rms_norm(leaf).float().pow(3).sum(), leaf, create_graph=True)
+        torch.autograd.grad(g.float().sum(), leaf)
+
+
+def test_gradients_of_two_leaves_are_apart(B):
+    from paper_1906_03707_amd import layers
+    a, b = (torch.randn(5, 8, device="cuda").requires_grad_() for _ in range(2))
+    layers.rms_norm(a, residual=b)[0].pow(3).sum().backward()
+    assert torch.equal(a.grad, b.grad) and a.grad.data_ptr() != b.grad.data_ptr()
+
+
+@pytest.mark.parametrize("d", [1, 31, 32, 100, 257])
+def test_quantized_rows_are_those_of_the_norm(B, d):
+    from paper_1906_03707_amd import layers
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    w = torch.randn(40, d, device="cuda", generator=gen) * torch.exp(4 * torch.randn(40, 1, device="cuda", generator=gen))
+    w[3] = 0
+    codes, scales = layers.quantize_fp8(w)
+    values = codes.double() * scales.double().repeat_interleave(32, 1)[:, :d]
+    s = scales.double().repeat_interleave(32, 1)[:, :d]
+    assert bool(((values - w.double()).abs() <= torch.maximum(w.double().abs() * 2.0 ** -4, s * 2.0 ** -10)).all()) and bool((scales[3].float() == 1).all())
+    # rows of +-4 have a root of 4: the norm's weight comes through exactly
+    sign = torch.randint(0, 2, (1, d), device="cuda", generator=gen) * 2.0 - 1
+    if d & (d - 1) == 0:
+        n, n_scales, _ = B.rms_norm_fp8(4 * sign, w[5].contiguous(), eps=0.0)
+        q, q_scales = layers.quantize_fp8(sign * w[5])
+        assert torch.equal(n.float(), q.float()) and torch.equal(n_scales.float(), q_scales.float())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_optimizer(B, bits):
+    """Against the formulas in 64 bits, or for 8 bits against binding.adamw; parameters without a gradient, gradients in another order of memory, saved states."""
+    from paper_1906_03707_amd import layers
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    make = lambda: [p.clone().requires_grad_() for p in start]   # noqa: E731
+    start = [torch.randn(33, 20, device="cuda", generator=gen), torch.randn(7, device="cuda", generator=gen), torch.randn(5, 4, device="cuda", generator=gen)]
+    grads = [[torch.randn(20, 33, device="cuda", generator=gen).t(), torch.randn(7, device="cuda", generator=gen)] for _ in range(4)]
+    ours, plain = make(), make()
+    opt = layers.AdamW(ours, lr=0.01, weight_decay=0.1, bits=bits, seed=3)
+    states = B.adamw_states(plain[:2], bits)
+    ref, m, v = [p.double() for p in start[:2]], [0, 0], [0, 0]
+    for t, gs in enumerate(grads, 1):
+        for p, g in zip(ours, gs):
+            p.grad = g
+        version = ours[0]._version
+        norm = opt.step(max_norm=1.0)
+        assert ours[0]._version > version and opt.steps == t
+        size = math.sqrt(sum(g.double().square().sum().item() for g in gs))
+        assert abs(norm.item() - size) <= 1e-6 * size and size > 1
+        B.adamw([p.detach() for p in plain[:2]], [g.contiguous() for g in gs], **states, step=t, lr=0.01, weight_decay=0.1, norm=norm, max_norm=1.0, seed=3)
+        for k, g in enumerate(gs):
+            g = g.double() / size
+            m[k], v[k] = 0.9 * m[k] + 0.1 * g, 0.999 * v[k] + 0.001 * g * g
+            ref[k] = ref[k] * (1 - 0.01 * 0.1) - 0.01 * (m[k] / (1 - 0.9 ** t)) / ((v[k] / (1 - 0.999 ** t)).sqrt() + 1e-8)
+        assert all(torch.equal(p, q) for p, q in zip(ours, plain))
+        if bits == 32:
+            assert all(near(p.detach(), q, 1e-6) for p, q in zip(ours, ref))
+    assert torch.equal(ours[2], start[2])
+    saved, more = opt.state_dict(), [p.detach().clone().requires_grad_() for p in ours]
+    other = layers.AdamW(more, lr=0.01, weight_decay=0.1, bits=bits)
+    other.load_state_dict(saved)
+    for o, ps in ((opt, ours), (other, more)):
+        for p, g in zip(ps, grads[0]):
+            p.grad = g
+        assert o.step() is None
+    assert all(torch.equal(p, q) for p, q in zip(ours, more))
+    opt.zero_grad()
+    assert all(p.grad is None for p in ours)
+    before = [p.detach().clone() for p in ours]
+    opt.step()                                             # no gradients: nothing to do
+    assert all(torch.equal(p, q) for p, q in zip(ours, before))
+    with pytest.raises(ValueError):
+        layers.AdamW(make(), bits=40 - bits).load_state_dict(saved)
+
+
+def make(B, d=20, rows=37, depth=3, classes=8, seed=0):
+    from paper_1906_03707_amd import synth
+    rowptr, col = synth.sbm(6, 40, 0.3, 0.01, seed=11)
+    n = rowptr.size - 1
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=gen)   # noqa: E731
+    params = [rnd(rows, d) * d ** -0.5]
+    for _ in range(depth):
+        params += [1 + 0.1 * rnd(d), 2 * rnd(d, d) * d ** -0.5]
+    params += [1 + 0.1 * rnd(d), rnd(d, classes) * d ** -0.5]
+    ids = torch.randint(-1, rows, (n,), device="cuda", generator=gen)
+    labels = torch.randint(0, classes, (n,), device="cuda", generator=gen)
+    labels[::5] = -100
+    adj = np.eye(n)
+    for u in range(n):
+        adj[u, col[rowptr[u]:rowptr[u + 1]]] += 1
+    adj = torch.from_numpy(adj / (np.diff(rowptr) + 1)[:, None]).cuda()
+    return B.hag_search(rowptr, col, n // 4).upload(), adj, params, ids, labels
+
+
+def logits64(adj, ids, params, padding):
+    """residual_gcn_logits with a dense matrix (A + I) / (degree + 1), in 64 bits."""
+    table, *rest = params
+    x = table[ids.clamp(min=0)] * table.shape[1] ** 0.5
+    x = torch.where((ids == padding)[:, None], 0.0, x)
+    for k in range(0, len(rest), 2):
+        z = adj @ (norm64(x, rest[k]) @ rest[k + 1])
+        x = x + torch.relu(z) if z.shape == x.shape else x
+    return z
+
+
+@pytest.mark.parametrize("d,depth", [(20, 3), (64, 1), (64, 6)])
+def test_loss_and_gradients(B, d, depth):
+    from paper_1906_03707_amd import layers
+    h, adj, params, ids, labels = make(B, d, depth=depth)
+    ours = [p.clone().requires_grad_() for p in params]
+    ref = [p.double().requires_grad_() for p in params]
+    z = layers.residual_gcn_logits(h, ids, ours, padding=-1)
+    loss, want = layers.softmax_loss(z, labels), torch.nn.functional.cross_entropy(logits64(adj, ids, ref, -1), labels)
+    assert abs(loss.item() - want.item()) <= 1e-5 * want.item()                    # the bars of the layer tests
+    loss.backward()
+    want.backward()
+    assert all(near(p.grad, q.grad, 1e-4) for p, q in zip(ours, ref))
+    naive = layers.residual_gcn_logits(h, ids, params, padding=-1, naive=True)
+    assert near(naive, z.detach(), 1e-5)
+
+
+def test_step(B):
+    from paper_1906_03707_amd import layers
+    h, adj, params, ids, labels = make(B)
+    ours = [p.clone().requires_grad_() for p in params]
+    opt = layers.AdamW(ours, lr=1e-3)
+    ref = [p.double().requires_grad_() for p in params]
+    m, v = [0] * len(ref), [0] * len(ref)
+    for t in (1, 2, 3):
+        loss, norm = layers.residual_gcn_step(h, ids, ours, labels, opt, max_norm=0.05, padding=-1)
+        want = torch.nn.functional.cross_entropy(logits64(adj, ids, ref, -1), labels)
+        grads = torch.autograd.grad(want, ref)
+        size = torch.sqrt(sum(g.square().sum() for g in grads)).item()
+        assert size > 0.05 and abs(loss.item() - want.item()) <= 1e-4 * want.item() and abs(norm.item() - size) <= 1e-3 * size
+        with torch.no_grad():
+            for k, (p, g) in enumerate(zip(ref, grads)):
+                g = g * (0.05 / size)
+                m[k], v[k] = 0.9 * m[k] + 0.1 * g, 0.999 * v[k] + 0.001 * g * g
+                p.copy_(p * (1 - 1e-5) - 1e-3 * (m[k] / (1 - 0.9 ** t)) / ((v[k] / (1 - 0.999 ** t)).sqrt() + 1e-8))
+    # an element whose gradient is all rounding moves by lr whatever its size: few do, by 3 lr at most
+    assert all(near(p.detach(), q.detach(), 1e-4) for p, q in zip(ours, ref))
+
+
+@pytest.mark.parametrize("d,depth", [(64, 2), (36, 3)])     # (aggregation takes widths that are multiples of 4)
+def test_serving_in_8_bits(B, d, depth):
+    from paper_1906_03707_amd import layers
+    h, adj, params, ids, _ = make(B, d, depth=depth)
+    served = layers.residual_gcn_fp8([p.clone().requires_grad_() for p in params])
+    z = layers.residual_gcn_logits_fp8(h, ids, served, padding=-1)
+    # the same calls one by one
+    x, update = layers.embedding(params[0], ids, d ** 0.5, -1), None
+    for k in range(1, len(params), 2):
+        codes, scales, x = B.rms_norm_fp8(x if update is None else update, params[k], residual=None if update is None else x)
+        q, q_scales = layers.quantize_fp8(params[k + 1].t().contiguous())
+        out = h.forward(B.fp8_product(codes, scales, q, q_scales), "gcn")
+        update = torch.relu(out)
+    assert torch.equal(z, out)
+    # every element of rows and matrices is off by at most 2^-4 of it, at random: a product by less than 2^-4 sqrt(2 / 3) of its norm, which layers then add to
+    want = logits64(adj, ids, [p.double() for p in params], -1)
+    assert near(z, want, 2.0 ** -4 * math.sqrt(2 / 3) * (depth + 1))
+    assert near(layers.residual_gcn_logits_fp8(h, ids, served, padding=-1, naive=True), want, 2.0 ** -4 * math.sqrt(2 / 3) * (depth + 1))
+
+
+def test_captured_serving(B):
+    from paper_1906_03707_amd import layers
+    h, _, params, ids, _ = make(B, 64, depth=2)
+    served = layers.residual_gcn_fp8(params)
+    run = lambda: layers.residual_gcn_logits_fp8(h, ids, served, padding=-1)   # noqa: E731
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        z = run()
+    for _ in range(4):
+        ids.copy_(ids.roll(7))
+        graph.replay()
+        assert torch.equal(z, run())
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_example(B, bits):
+    sys.path.insert(0, os.path.join(ROOT, "examples"))
+    try:
+        import residual_gcn
+    finally:
+        sys.path.pop(0)
+    results = residual_gcn.main(["--blocks", "8", "--block", "48", "--steps", "12", "--bits", str(bits)])
+    assert len(results) == 3 and all(math.isfinite(r) for r in results)
