@@ -13,7 +13,7 @@ namespace hag {
 
 // The tensors are cut into units of at most `unit` elements, one workgroup each; a launch takes as many tensors as its argument block holds.
 constexpr int kAdamTensors = 48;
-constexpr int64_t kAdamUnits = 4096, kAdamRound = 4096;
+constexpr int64_t kAdamUnits = 4096, kAdamRound = 1024;
 struct AdamArgs {
     struct Tensor {
         void *param;

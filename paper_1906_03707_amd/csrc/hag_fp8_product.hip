@@ -242,15 +242,33 @@ __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(Produc
 
 // ------------------------------------------------------------------------------------------------ few rows, or rows at any address
 
-// 16 columns from `col` of a row at any address, zeros from column d on
-__device__ __forceinline__ bytes16_t load16(const uint8_t *row, int col, int d) {
+// 16 columns from `col` of a row at any address, zeros from column d on; begin, end: of the matrix in memory.  Where 16 bytes from there are not all the matrix's, its last 16 are read and
+// moved (a matrix of fewer is read byte by byte).
+__device__ __forceinline__ bytes16_t load16(const uint8_t *row, int col, int d, const uint8_t *begin, const uint8_t *end) {
     bytes16_t v = {};
-    if (col + 16 <= d) {
-        v = *reinterpret_cast<const bytes16_t *>(row + col);
-    } else if (col < d) {
+    const int have = d - col;
+    if (have <= 0) return v;
+    const uint8_t *from = row + col;
+    if (have >= 16 || end - begin >= 16) {
+        const int over = max((int)min(from + 16 - end, (ptrdiff_t)16), 0) * 8;     // bits that lie beyond the end
+        v = *reinterpret_cast<const bytes16_t *>(over > 0 ? end - 16 : from);
+        if (have < 16) {
+            uint64_t low = v[0] | (uint64_t)v[1] << 32, high = v[2] | (uint64_t)v[3] << 32;
+            if (over > 0) {
+                low = over >= 64 ? high >> (over - 64) : low >> over | high << (64 - over);
+                high = over >= 64 ? 0 : high >> over;
+            }
+            low &= have >= 8 ? ~0ull : (1ull << 8 * have) - 1;
+            high &= have <= 8 ? 0 : (1ull << 8 * (have - 8)) - 1;
+            v[0] = (uint32_t)low;
+            v[1] = (uint32_t)(low >> 32);
+            v[2] = (uint32_t)high;
+            v[3] = (uint32_t)(high >> 32);
+        }
+    } else {
 #pragma unroll
         for (int i = 0; i < 15; ++i)
-            if (col + i < d) v[i / 4] |= (uint32_t)row[col + i] << 8 * (i % 4);
+            if (i < have) v[i / 4] |= (uint32_t)row[col + i] << 8 * (i % 4);
     }
     return v;
 }
@@ -259,10 +277,16 @@ template <bool WIDE>
 struct Raw {
     bytes16_t a, b;
     uint32_t scales;
-    __device__ __forceinline__ void load(const uint8_t *row, const uint8_t *of, int col, int q, int d) {
+    __device__ __forceinline__ void load(const uint8_t *row, const uint8_t *of, int col, int q, int d, const uint8_t *begin, const uint8_t *end) {
         const int block = col / kScaleBlock;
-        a = load16(row, col + 16 * q, d);
-        b = load16(row, col + 64 + 16 * q, d);
+        if (col + 128 <= d) {
+            a = *reinterpret_cast<const bytes16_t *>(row + col + 16 * q);
+            b = *reinterpret_cast<const bytes16_t *>(row + col + 64 + 16 * q);
+            scales = WIDE ? (uint32_t)of[block + q / 2] | (uint32_t)of[block + 2 + q / 2] << 8 : of[block + q];
+            return;
+        }
+        a = load16(row, col + 16 * q, d, begin, end);
+        b = load16(row, col + 64 + 16 * q, d, begin, end);
         scales = WIDE ? load_scale(of, block + q / 2, d) | load_scale(of, block + 2 + q / 2, d) << 8 : load_scale(of, block + q, d);
     }
     __device__ __forceinline__ operator Part<WIDE>() const { return Part<WIDE>(a, b, scales); }
@@ -273,9 +297,10 @@ template <typename O, int R>
 __global__ __launch_bounds__(R == 1 ? 1024 : 512) void product_split_kernel(ProductArgs a) {
     constexpr bool WIDE = sizeof(O) == 4;
     __shared__ float4 sums[(R == 1 ? 16 : 8) * R * 2 * kWave];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave, r = lane % 16, q = lane / 16;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), waves = blockDim.x / kWave, r = lane % 16, q = lane / 16;
     const int64_t row0 = (int64_t)blockIdx.x * (16 * R), col0 = (int64_t)blockIdx.y * 32;
     const uint8_t *x[R], *x_scales[R], *w[2], *w_scales[2];
+    const uint8_t *x_end = a.x + (a.n - 1) * a.x_stride + a.d, *w_end = a.w + (a.k - 1) * a.w_stride + a.d;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int64_t row = min(row0 + i * 16 + r, a.n - 1);
@@ -296,9 +321,9 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void product_split_kernel(Prod
     Raw<WIDE> rx[R], rw[2];
     auto load = [&](int col) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) rw[t].load(w[t], w_scales[t], col, q, a.d);
+        for (int t = 0; t < 2; ++t) rw[t].load(w[t], w_scales[t], col, q, a.d, a.w, w_end);
 #pragma unroll
-        for (int i = 0; i < R; ++i) rx[i].load(x[i], x_scales[i], col, q, a.d);
+        for (int i = 0; i < R; ++i) rx[i].load(x[i], x_scales[i], col, q, a.d, a.x, x_end);
     };
     int col = wave * 128;
     if (col < a.d) load(col);
@@ -393,8 +418,9 @@ int hag_fp8_product(int64_t n, int64_t d, int64_t k, const uint8_t *x, int64_t x
         // 1000 x 2048 x 300 15.8, 13.1, 11.1, 14.0; but 2048 x 512 x 512 10.5, 7.9, 6.9, 6.2 and 300 x 2048 x 2048 25.9, 19.3, 20.8, 14.4.
         const int64_t groups = (k + 31) / 32, tiles = ((n + 127) / 128) * ((k + 127) / 128);
         if ((n + 15) / 16 * groups <= 256) return launch_split<O, 1>(a, s);
-        if ((n + 31) / 32 * groups * d <= 400000) return launch_split<O, 2>(a, s);
+        if (tiles <= 64 && (n + 31) / 32 * groups * d <= 400000) return launch_split<O, 2>(a, s);
         if (!aligned || tiles <= 24) return launch_split<O, 4>(a, s);
+        if (k <= 64) return launch_tiles<O, 128, 64, 4, 1>(a, s);
         if (n * k < (int64_t)1 << 24 || k <= 128) return launch_tiles<O, 128, 128, 2, 2>(a, s);
         if constexpr (sizeof(O) == 2) return launch_tiles<O, 256, 256, 2, 4>(a, s);
         else return launch_tiles<O, 256, 128, 4, 2>(a, s);
