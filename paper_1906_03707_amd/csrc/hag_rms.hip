@@ -153,10 +153,15 @@ __global__ __launch_bounds__(kNormBlock<LPR>) void rms_kernel(RmsArgs a) {
                 continue;
             }
             constexpr int kLanes = LPR < kScaleBlock / V ? LPR : kScaleBlock / V;   // of a block
-            float most = 0.f;
+            uint32_t most = 0;                             // as whole numbers, those that are none are above all others
 #pragma unroll
-            for (int e = 0; e < V; ++e) most = fmaxf(most, (TAIL ? col + e : col) < a.d ? finite_amount(y[e]) : 0.f);
-            const uint32_t byte = scale_byte(lanes_max<kLanes>(most));
+            for (int e = 0; e < V; ++e) most = max(most, (TAIL ? col + e : col) < a.d ? __float_as_uint(y[e]) & 0x7fffffffu : 0u);
+            if (__any(most >= 0x7f800000u)) {
+                most = 0;
+#pragma unroll
+                for (int e = 0; e < V; ++e) most = max(most, (TAIL ? col + e : col) < a.d ? __float_as_uint(finite_amount(y[e])) : 0u);
+            }
+            const uint32_t byte = scale_byte(lanes_max<kLanes>(__uint_as_float(most)));
             const float by = scale_inverse(byte);
             if (!here) continue;
             uint32_t code[V / 4];
@@ -482,13 +487,22 @@ static int rms_args(int64_t n, int64_t d, hag_dtype_t dtype, const void *x, int6
     return HAG_OK;
 }
 
+// Rows whose output has 8 bits are bound by instructions rather than bytes: half a wavefront, of two vectors a lane, halves what is done once a lane and row (56944 x 251 fp32 18.5 -> 16.3 us,
+// x 256 14.3 -> 13.8; fewer lanes for shorter rows gain nothing: 232965 x 100 22.7 -> 23.9).
+static NormShape rms_shape(int64_t d, int vec, bool out8) {
+    const NormShape s = norm_shape(d, vec);
+    return out8 && s.lpr == kWave && s.k == 1 ? NormShape{kWave / 2, 2} : s;
+}
+
 template <bool OUT8>
 static int rms_forward(const RmsArgs &a, hag_dtype_t dtype, hipStream_t stream) {
     return elem_switch(dtype, [&](auto e) {
         using T = decltype(e);
-        const NormShape s = norm_shape(a.d, kVec<T>);
+        const NormShape s = rms_shape(a.d, kVec<T>, OUT8);
         if (s.k == 0) return rms_launch<T>(rms_wide_kernel<T, OUT8>, a, 1, kWide, stream);
-        const rms_kernel_t kernel = a.d % kVec<T> ? norm_pick<rms_kernel_t, T, RmsForward<T, true, OUT8>::template Of>(s) : norm_pick<rms_kernel_t, T, RmsForward<T, false, OUT8>::template Of>(s);
+        rms_kernel_t kernel;
+        if (OUT8 && s.lpr == kWave / 2 && s.k == 2) kernel = a.d % kVec<T> ? RmsForward<T, true, true>::template Of<32, 2>::kernel : RmsForward<T, false, true>::template Of<32, 2>::kernel;
+        else kernel = a.d % kVec<T> ? norm_pick<rms_kernel_t, T, RmsForward<T, true, OUT8>::template Of>(s) : norm_pick<rms_kernel_t, T, RmsForward<T, false, OUT8>::template Of>(s);
         return rms_launch<T>(kernel, a, norm_side(s, false) * rms_rows(s.lpr, s.k, kVec<T>), norm_block(s, false), stream);
     });
 }
