@@ -258,6 +258,8 @@ __device__ __forceinline__ void adam_unit(const AdamArgs::Tensor &t, const AdamN
     }
 }
 
+// Bound by moving parameters, gradients and states: 30 M fp32 parameters with states in 32 bits 167 us (28 bytes each, 5.0 TB/s; one or four pieces on their way 167 and 165, streaming stores
+// 168), in 8 bits with bf16 gradients and copies 101 (16.1 bytes, 4.8; 75 vector instructions an element, which issue for seven tenths of the time, 12 of them the hash).
 template <int BITS>
 __global__ __launch_bounds__(kBlock) void adamw_kernel(AdamArgs a) {
     AdamNumbers s;

@@ -117,7 +117,14 @@ struct ProductTiles {
     int32_t col_tiles, tiles;
 };
 
-// A workgroup takes TM rows of x and TN of w, its wavefronts WR times WC parts of them.  128 columns of both are on their way from memory to LDS while the 128 before are multiplied.
+// A workgroup takes TM rows of x and TN of w, its wavefronts WR times WC parts of them.  128 columns of both are on their way from memory to LDS, past the registers, while the 128 before are
+// multiplied; the first two sets are requested together.  What LDS holds and the registers' sums limit the tile: 256 x 256 for results of 16 bits (64 KB for 128 columns, two of them; 128
+// registers of sums).
+// 131072 x 1024 x 1024 into bf16 200 us (1.4 PFLOP/s; the library's bf16 product of these sizes 307 us), without the products 190, without the stores 142, without the loads 163: loads come 2 us
+// after they are asked for, and only as much is on its way as LDS has room for.  128 columns as two 64s, so that two workgroups fit a compute unit, took 266 (lines of 128 bytes are asked for
+// twice, what L2 answers per clock), one workgroup that goes from tile to tile and asks for the next one's first columns early 212, tiles of 128 x 128 259.
+// Narrow results are bound by memory: 232965 x 128 x 128 into bf16 17.7 us (5.1 TB/s), into fp32 29.5 (5.1), 56944 x 251 x 74 into fp32 10.9 (2.9: a load's way, a product's, a store's).
+// fp32 results convert in registers: 131072 x 1024 x 1024 390 us (0.7 PFLOP/s).
 template <typename O, int TM, int TN, int WR, int WC>
 __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(ProductTiles args) {
     constexpr bool WIDE = sizeof(O) == 4;
@@ -148,8 +155,8 @@ __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(Produc
         const int row = min(i * THREADS + (int)threadIdx.x, ROWS - 1);
         scale_row[i] = row < TM ? a.x_scales + (row0 + min(row, x_rows - 1)) * a.x_scales_stride : a.w_scales + (col0 + min(row - TM, w_rows - 1)) * a.w_scales_stride;
     }
-    uint32_t scale[SCALES];
-    auto request = [&](int step, bytes16_t *codes) {
+    uint32_t scale0[SCALES], scale1[SCALES];
+    auto request = [&](int step, bytes16_t *codes, uint32_t (&scale)[SCALES]) {
         const uint8_t *from_x = x + (int64_t)step * 128, *from_w = w + (int64_t)step * 128;
         auto load = [&](const uint8_t *from, int i) {
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)(codes + i * THREADS + wave * kWave), 16, 0, 0);
@@ -174,7 +181,7 @@ __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(Produc
             }
         }
     };
-    auto keep_scales = [&](uint32_t *scales) {
+    auto keep_scales = [&](uint32_t *scales, const uint32_t (&scale)[SCALES]) {
 #pragma unroll
         for (int i = 0; i < SCALES; ++i)
             if (SCALES * THREADS == ROWS || i * THREADS + (int)threadIdx.x < ROWS) scales[i * THREADS + threadIdx.x] = scale[i];
@@ -219,17 +226,18 @@ __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(Produc
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto turn = [&](int step, bytes16_t *codes, uint32_t *scales, bytes16_t *next) {
+    auto turn = [&](int step, bytes16_t *codes, uint32_t *scales, const uint32_t (&scale)[SCALES], bytes16_t *next, uint32_t (&next_scale)[SCALES]) {
         if (step + 1 == steps && a.d % 16) cut(step, codes);
-        keep_scales(scales);
+        keep_scales(scales, scale);
         __syncthreads();
-        if (step + 1 < steps) request(step + 1, next);
+        if (step > 0 && step + 1 < steps) request(step + 1, next, next_scale);
         work(codes, scales);
     };
-    request(0, codes0);
+    request(0, codes0, scale0);
+    if (steps > 1) request(1, codes1, scale1);             // (both are empty: two waits become one)
     for (int step = 0; step < steps; step += 2) {
-        turn(step, codes0, scales0, codes1);
-        if (step + 1 < steps) turn(step + 1, codes1, scales1, codes0);
+        turn(step, codes0, scales0, scale0, codes1, scale1);
+        if (step + 1 < steps) turn(step + 1, codes1, scales1, scale1, codes0, scale0);
     }
     const int64_t col = col0 + wc * (TN / WC);
     const int have = (int)max((int64_t)0, min(a.k - col, (int64_t)(TN / WC)));
@@ -292,7 +300,8 @@ struct Raw {
     __device__ __forceinline__ operator Part<WIDE>() const { return Part<WIDE>(a, b, scales); }
 };
 
-// A workgroup takes 16 * R rows of x and 32 of w, its wavefronts every so many 128 columns of them, straight from memory; their sums are added up in LDS in their order.
+// A workgroup takes 16 * R rows of x and 32 of w, its wavefronts every so many 128 columns of them, straight from memory; their sums are added up in LDS in their order.  Bound by the way
+// of one load after the other to the end: 1 x 512 x 512 3.3 us, 1 x 2048 x 2048 5.5 (0.8 TB/s of weights).
 template <typename O, int R>
 __global__ __launch_bounds__(R == 1 ? 1024 : 512) void product_split_kernel(ProductArgs a) {
     constexpr bool WIDE = sizeof(O) == 4;

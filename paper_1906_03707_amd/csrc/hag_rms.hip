@@ -76,7 +76,8 @@ __device__ __forceinline__ void rms_far_row(const RmsArgs &a, int64_t row, float
     if (l == 0 && a.rstd) a.rstd[row] = r * scale;
 }
 
-// Bound by reading x and the residual and writing their sum and y.  Every lane requests R rows one after the other before it needs the first.
+// Bound by reading x and the residual and writing their sum and y.  Every lane requests R rows one after the other before it needs the first.  232965 x 128 bf16 with residual 37 us (6.4 TB/s),
+// without 19.8 (6.0), 56944 x 251 fp32 20.0 (5.7).  In 8 bits 232965 x 256 bf16 with residual 75 us (5.6), 56944 x 251 fp32 16.5 (4.4: nine tenths of the time instructions issue).
 template <typename T, int LPR, int K, int R, bool TAIL, bool OUT8>
 __global__ __launch_bounds__(kNormBlock<LPR>) void rms_kernel(RmsArgs a) {
     __shared__ float2 lds[2][16];
@@ -267,7 +268,7 @@ struct RmsGradArgs {
 };
 
 // Bound by reading h, g_y and g_h and writing g_x.  Workgroups take rows in turn, keep the sums of their columns for g_w in registers, and leave them in `partial`, added up in a fixed
-// order by rms_reduce_kernel.  The next rows are requested before the present ones are worked on.
+// order by rms_reduce_kernel.  The next rows are requested before the present ones are worked on.  65536 x 512 fp32 with g_h 100 us with the last sums (5.3 TB/s), 56944 x 251 bf16 20.7 (4.1).
 template <typename T, int LPR, int K, int R, bool TAIL>
 __global__ __launch_bounds__(kGradBlock<LPR>) void rms_grad_kernel(RmsGradArgs a) {
     extern __shared__ float sums[];                        // [wavefronts][LPR * K * V], rows of up to 64 lanes
