@@ -174,7 +174,7 @@ def quantize_fp8(w):
     """Rows [k, d] in 8 bits, as rms_norm_fp8 leaves them: (codes, scales), a power of two for every 32 columns, elements to the nearest.  Plain torch: for weights, once."""
     k, d = w.shape
     w = w.float()
-    most = torch.nn.functional.pad(w.abs(), (0, -d % 32)).reshape(k, (d + 31) // 32, 32).amax(2)
+    most = torch.nn.functional.pad(torch.where(w.isfinite(), w.abs(), 0.0), (0, -d % 32)).reshape(k, (d + 31) // 32, 32).amax(2)
     fraction, exponent = torch.frexp(most)
     e = torch.where(fraction == 0, 0, (exponent - 9 + (fraction > 0.875)).clamp(min=-127))                 # the smallest with most <= 448 * 2^e
     codes = torch.zeros(k, (d + 15) // 16 * 16, dtype=torch.float8_e4m3fn, device=w.device)
@@ -206,16 +206,16 @@ class AdamW:
 
     def step(self, max_norm=None):
         """One step on the parameters that have a gradient.  max_norm: as if their gradients were scaled down to that norm, which they are not; the norm they have, a float32 scalar on
-        the device, is returned (nothing waits for it), and where it is no finite number no parameter and no state changes."""
+        the device, is returned (nothing waits for it), and where it is no finite number no parameter and no state changes (a NaN among the gradients makes all of them NaN)."""
         at = [i for i, p in enumerate(self.params) if p.grad is not None]
         params = [self.params[i] for i in at]
         grads = [p.grad if p.grad.stride() == p.stride() or p.is_contiguous() and p.grad.is_contiguous() else torch.empty_like(p, dtype=p.grad.dtype).copy_(p.grad) for p in params]
         norm = None if max_norm is None else binding.clip_gradients(grads, float("inf"))
-        self.steps += 1
-        binding.adamw([p.detach() for p in params], grads, **{k: [x[i] for i in at] for k, x in self.states.items()}, step=self.steps, lr=self.lr, betas=self.betas, eps=self.eps,
-                      weight_decay=self.weight_decay, norm=norm, max_norm=max_norm, seed=self.seed)
         if params:
+            binding.adamw([p.detach() for p in params], grads, **{k: [x[i] for i in at] for k, x in self.states.items()}, step=self.steps + 1, lr=self.lr, betas=self.betas, eps=self.eps,
+                          weight_decay=self.weight_decay, norm=norm, max_norm=max_norm, seed=self.seed)
             torch.autograd.graph.increment_version(params)
+            self.steps += 1
         return norm
 
     def state_dict(self):

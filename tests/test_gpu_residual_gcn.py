@@ -78,6 +78,10 @@ def test_quantized_rows_are_those_of_the_norm(B, d):
     gen = torch.Generator(device="cuda").manual_seed(d)
     w = torch.randn(40, d, device="cuda", generator=gen) * torch.exp(4 * torch.randn(40, 1, device="cuda", generator=gen))
     w[3] = 0
+    broken = w.clone()
+    broken[1, 0], broken[2, d - 1] = float("inf"), float("nan")
+    codes, scales = layers.quantize_fp8(broken)
+    assert torch.equal(codes.float().isnan(), ~broken.isfinite()) and bool((scales.float() > 0).all())
     codes, scales = layers.quantize_fp8(w)
     values = codes.double() * scales.double().repeat_interleave(32, 1)[:, :d]
     s = scales.double().repeat_interleave(32, 1)[:, :d]
@@ -130,8 +134,12 @@ def test_optimizer(B, bits):
     opt.zero_grad()
     assert all(p.grad is None for p in ours)
     before = [p.detach().clone() for p in ours]
-    opt.step()                                             # no gradients: nothing to do
-    assert all(torch.equal(p, q) for p, q in zip(ours, before))
+    steps = opt.steps
+    assert opt.step() is None and opt.step(max_norm=1.0).item() == 0               # no gradients: nothing to do
+    assert all(torch.equal(p, q) for p, q in zip(ours, before)) and opt.steps == steps
+    ours[1].grad = torch.ones(7, device="cuda")
+    ours[1].grad[3] = float("nan")
+    assert opt.step(max_norm=1.0).isnan() and all(torch.equal(p, q) for p, q in zip(ours, before))
     with pytest.raises(ValueError):
         layers.AdamW(make(), bits=40 - bits).load_state_dict(saved)
 
