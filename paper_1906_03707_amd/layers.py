@@ -192,9 +192,15 @@ def clip_gradients(parameters, max_norm):
     return norm
 
 
+def _no_capture():
+    if torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("an optimiser's step counts on the host and cannot be captured: binding.adamw takes the number from the device")
+
+
 class AdamW:
     """AdamW (hag_adamw) for float32, bfloat16 or float16 leaves.  bits: of its states, 32 (two float32 numbers for each element) or 8 (two bytes and a sixteenth, rounded by chance from `seed` and
-    the step so that their means are kept).  lr may be changed between steps; one count of steps for all parameters."""
+    the step so that their means are kept).  lr may be changed between steps; one count of steps for all parameters.  A step is not captured into a graph, whose replays would all have its
+    number: binding.adamw takes the number, and lr, from the device."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, seed=0):
         self.params, self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.seed, self.steps = list(params), lr, betas, eps, weight_decay, bits, seed, 0
@@ -207,6 +213,7 @@ class AdamW:
     def step(self, max_norm=None):
         """One step on the parameters that have a gradient.  max_norm: as if their gradients were scaled down to that norm, which they are not; the norm they have, a float32 scalar on
         the device, is returned (nothing waits for it), and where it is no finite number no parameter and no state changes (a NaN among the gradients makes all of them NaN)."""
+        _no_capture()
         at = [i for i, p in enumerate(self.params) if p.grad is not None]
         params = [self.params[i] for i in at]
         grads = [p.grad if p.grad.stride() == p.stride() or p.is_contiguous() and p.grad.is_contiguous() else torch.empty_like(p, dtype=p.grad.dtype).copy_(p.grad) for p in params]
@@ -360,6 +367,7 @@ def residual_gcn_logits(h, ids, params, padding=None, naive=False):
 
 def residual_gcn_step(h, ids, params, labels, optimizer, max_norm=None, padding=None):
     """One step of an AdamW over `params` on the SoftMax loss of residual_gcn_logits; (loss, gradient norm or None), scalars on the device."""
+    _no_capture()
     optimizer.zero_grad()
     loss = softmax_loss(residual_gcn_logits(h, ids, params, padding), labels)
     loss.backward()

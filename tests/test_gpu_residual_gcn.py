@@ -249,6 +249,25 @@ def test_captured_serving(B):
         torch.cuda.synchronize()
 
 
+def test_optimizer_refuses_capture(B):
+    from paper_1906_03707_amd import layers
+    p = torch.ones(40, device="cuda", requires_grad=True)
+    p.grad = torch.ones(40, device="cuda")
+    opt = layers.AdamW([p])
+    opt.step()
+    before, x = p.detach().clone(), torch.zeros(8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x += 1
+        with pytest.raises(RuntimeError, match="captured"):
+            opt.step()
+        with pytest.raises(RuntimeError, match="captured"):
+            layers.residual_gcn_step(None, None, [p], None, opt)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(p.detach(), before) and opt.steps == 1 and p.grad is not None and float(x.sum()) == 8
+
+
 @pytest.mark.parametrize("bits", [8, 32])
 def test_example(B, bits):
     sys.path.insert(0, os.path.join(ROOT, "examples"))
