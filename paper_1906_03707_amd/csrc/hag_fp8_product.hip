@@ -258,7 +258,7 @@ __device__ __forceinline__ bytes16_t load16(const uint8_t *row, int col, int d, 
     if (have <= 0) return v;
     const uint8_t *from = row + col;
     if (have >= 16 || end - begin >= 16) {
-        const int over = (int)max(min(from + 16 - end, (ptrdiff_t)16), (ptrdiff_t)0) * 8;      // bits that lie beyond the end
+        const int over = from > end - 16 ? (int)(from - (end - 16)) * 8 : 0;          // bits that lie beyond the end, 120 at most: from is before it
         v = *reinterpret_cast<const bytes16_t *>(over > 0 ? end - 16 : from);
         if (have < 16) {
             uint64_t low = v[0] | (uint64_t)v[1] << 32, high = v[2] | (uint64_t)v[3] << 32;
