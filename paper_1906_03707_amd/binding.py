@@ -11,6 +11,7 @@ from __future__ import annotations
 import array
 import ctypes
 import os
+import sys
 
 import numpy as np
 
@@ -210,6 +211,19 @@ def _dev_ptr(t):
     return ctypes.c_void_p(t.data_ptr())
 
 
+_ended = []                                 # (free, handle) of objects that are gone
+
+
+def _free_ended(*more):
+    """Frees the handles of objects that are gone; not while a graph is captured, which giving memory back would break (garbage is collected at any time): with the next ones then."""
+    _ended.extend(more)
+    torch = sys.modules.get("torch")
+    if _ended and not (torch is not None and torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing()):
+        while _ended:
+            free, handle = _ended.pop()
+            free(handle)
+
+
 class Hag:
     """Owner of one hag_t handle."""
 
@@ -222,8 +236,8 @@ class Hag:
     def __del__(self):
         try:
             if self._h:
-                lib().hag_free(self._h)
-                self._h = None
+                handle, self._h = self._h, None
+                _free_ended((lib().hag_free, handle))
         except Exception:
             pass
 
@@ -259,6 +273,7 @@ class Hag:
 
     # ---- device side -------------------------------------------------------------------------
     def upload(self):
+        _free_ended()
         _check(lib().hag_upload(self._h, _stream_ptr()))
         return self
 
@@ -942,8 +957,8 @@ class SeqHag:
     def __del__(self):
         try:                                # at interpreter shutdown the module's globals may be gone already
             if getattr(self, "_h", None):
-                lib().hag_seq_free(self._h)
-                self._h = None
+                handle, self._h = self._h, None
+                _free_ended((lib().hag_seq_free, handle))
         except Exception:
             pass
 

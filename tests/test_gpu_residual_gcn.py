@@ -249,6 +249,27 @@ def test_captured_serving(B):
         torch.cuda.synchronize()
 
 
+def test_handles_that_end_during_a_capture(B):
+    from paper_1906_03707_amd import layers
+    h, _, params, ids, _ = make(B, 64, depth=2)
+    ends = [make(B, 64, depth=2)[0] for _ in range(2)]
+    served = layers.residual_gcn_fp8(params)
+    want = layers.residual_gcn_logits_fp8(h, ids, served, padding=-1)
+    B._free_ended()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ends.pop()                                         # as the garbage collection might
+        z = layers.residual_gcn_logits_fp8(h, ids, served, padding=-1)
+        ends.pop()
+    assert len(B._ended) >= 2
+    for _ in range(3):
+        z.zero_()
+        graph.replay()
+        assert torch.equal(z, want)
+    make(B, 64, depth=2)
+    assert not B._ended
+
+
 def test_optimizer_refuses_capture(B):
     from paper_1906_03707_amd import layers
     p = torch.ones(40, device="cuda", requires_grad=True)
