@@ -249,6 +249,56 @@ def test_captured_serving(B):
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_captured_training(B, bits):
+    """Forward, backward, the gradients' norm and a step whose number is on the device, replayed, against the same steps one by one."""
+    from paper_1906_03707_amd import layers
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    start = [torch.randn(300, 96, device="cuda", generator=gen), 1 + 0.1 * torch.randn(96, device="cuda", generator=gen), 1 + 0.1 * torch.randn(96, device="cuda", generator=gen)]
+    update, gy, gx = (torch.randn(300, 96, device="cuda", generator=gen) for _ in range(3))
+
+    def backward(params):
+        for p in params:
+            p.grad = None
+        x, w1, w2 = params
+        y = layers.rms_norm(x, w1)
+        z, h = layers.rms_norm(y * update, w2, residual=x)
+        torch.autograd.backward([z, h], [gy, gx])
+
+    def whole(params, states, step):
+        backward(params)
+        grads = [p.grad for p in params]
+        norm = B.clip_gradients(grads, float("inf"))
+        step += 1
+        B.adamw([p.detach() for p in params], grads, **states, step=step, lr=0.01, weight_decay=0.1, norm=norm, max_norm=1.0, seed=5)
+        return norm
+
+    ours, step = [p.clone().requires_grad_() for p in start], torch.zeros((), dtype=torch.int64, device="cuda")
+    states = B.adamw_states(ours, bits)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        whole(ours, states, step)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm = whole(ours, states, step)
+    again = [p.clone().requires_grad_() for p in start]
+    opt = layers.AdamW(again, lr=0.01, weight_decay=0.1, bits=bits, seed=5)
+    backward(again)
+    opt.step(max_norm=1.0)
+    for t in range(4):
+        graph.replay()
+        backward(again)
+        assert torch.equal(norm, opt.step(max_norm=1.0))
+        assert all(torch.equal(p.detach(), q.detach()) for p, q in zip(ours, again))
+        for k, x in states.items():
+            assert all(torch.equal(u.view(torch.uint8), v.view(torch.uint8)) for u, v in zip(x, opt.states[k]))
+        update.mul_(1.01)
+        torch.cuda.synchronize()
+    assert int(step) == opt.steps == 5
+
+
 def test_handles_that_end_during_a_capture(B):
     from paper_1906_03707_amd import layers
     h, _, params, ids, _ = make(B, 64, depth=2)
