@@ -178,7 +178,8 @@ def quantize_fp8(w):
     fraction, exponent = torch.frexp(most)
     e = torch.where(fraction == 0, 0, (exponent - 9 + (fraction > 0.875)).clamp(min=-127))                 # the smallest with most <= 448 * 2^e
     codes = torch.zeros(k, (d + 15) // 16 * 16, dtype=torch.float8_e4m3fn, device=w.device)
-    codes[:, :d] = torch.ldexp(w, -e.repeat_interleave(32, 1)[:, :d]).to(torch.float8_e4m3fn)
+    inverse = ((127 - e.int()) << 23).view(torch.float32)  # (torch.ldexp's powers of two are a unit off on the device: ties would be none)
+    codes[:, :d] = (w * inverse.repeat_interleave(32, 1)[:, :d]).to(torch.float8_e4m3fn)
     return codes[:, :d], (e + 127).to(torch.uint8).view(torch.float8_e8m0fnu)
 
 

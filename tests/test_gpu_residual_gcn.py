@@ -8,6 +8,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
+E4M3 = torch.float8_e4m3fn
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
@@ -92,6 +93,22 @@ def test_quantized_rows_are_those_of_the_norm(B, d):
         n, n_scales, _ = B.rms_norm_fp8(4 * sign, w[5].contiguous(), eps=0.0)
         q, q_scales = layers.quantize_fp8(sign * w[5])
         assert torch.equal(n.float(), q.float()) and torch.equal(n_scales.float(), q_scales.float())
+
+
+def test_quantized_ties(B):
+    """Numbers half way between two codes, at every scale, go to the even one; the codes' own numbers stay."""
+    from paper_1906_03707_amd import layers
+    codes = torch.arange(126, dtype=torch.uint8, device="cuda").view(E4M3).double()
+    half = (codes[1:] + codes[:-1]) / 2
+    # blocks of 32: the largest code's number, then 31 of the others
+    row = torch.cat([torch.cat([codes.new_tensor([448.0]), part]) for part in torch.cat([codes, half]).split(31)])
+    exponents = torch.arange(-110, 119, device="cuda")
+    w = (row * 2.0 ** exponents.double().cpu()[:, None].cuda()).float()
+    got, scales = layers.quantize_fp8(w)
+    assert torch.equal(scales.view(torch.uint8)[:, 0].long(), exponents + 127) and torch.equal(scales.view(torch.uint8), scales.view(torch.uint8)[:, :1].expand(scales.shape))
+    # (the rows' numbers have few bits: whole multiples of 2^-10)
+    want = row.float().cpu().to(E4M3).view(torch.uint8).cuda()
+    assert torch.equal(got.contiguous().view(torch.uint8), want.expand(got.shape))
 
 
 @pytest.mark.parametrize("bits", [32, 8])
