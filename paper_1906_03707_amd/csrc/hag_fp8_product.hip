@@ -124,7 +124,7 @@ struct ProductTiles {
 // after they are asked for, and only as much is on its way as LDS has room for.  128 columns as two 64s, so that two workgroups fit a compute unit, took 266 (lines of 128 bytes are asked for
 // twice, what L2 answers per clock), one workgroup that goes from tile to tile and asks for the next one's first columns early 212, tiles of 128 x 128 259.
 // Narrow results are bound by memory: 232965 x 128 x 128 into bf16 17.7 us (5.1 TB/s), into fp32 29.5 (5.1), 56944 x 251 x 74 into fp32 10.9 (2.9: a load's way, a product's, a store's).
-// fp32 results convert in registers: 131072 x 1024 x 1024 390 us (0.7 PFLOP/s).
+// fp32 results convert in registers: 131072 x 1024 x 1024 362 us (0.76 PFLOP/s; with the next piece converted between the products of the present one 364), 16384 x 2048 x 2048 148 (0.93).
 template <typename O, int TM, int TN, int WR, int WC>
 __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(ProductTiles args) {
     constexpr bool WIDE = sizeof(O) == 4;
@@ -430,9 +430,10 @@ int hag_fp8_product(int64_t n, int64_t d, int64_t k, const uint8_t *x, int64_t x
         if (tiles <= 64 && (n + 31) / 32 * groups * d <= 400000) return launch_split<O, 2>(a, s);
         if (!aligned || tiles <= 24) return launch_split<O, 4>(a, s);
         if (k <= 64) return launch_tiles<O, 128, 64, 4, 1>(a, s);
-        if (n * k < (int64_t)1 << 24 || k <= 128) return launch_tiles<O, 128, 128, 2, 2>(a, s);
-        if constexpr (sizeof(O) == 2) return launch_tiles<O, 256, 256, 2, 4>(a, s);
-        else return launch_tiles<O, 256, 128, 4, 2>(a, s);
+        // (fp32 results: 256 x 128 takes 392 us for 131072 x 1024 x 1024, 128 x 128 362; 16384 x 2048 x 2048 148 both)
+        if constexpr (sizeof(O) == 2)
+            if (n * k >= (int64_t)1 << 24 && k > 128) return launch_tiles<O, 256, 256, 2, 4>(a, s);
+        return launch_tiles<O, 128, 128, 2, 2>(a, s);
     });
 }
 
