@@ -76,8 +76,8 @@ __device__ __forceinline__ void rms_far_row(const RmsArgs &a, int64_t row, float
     if (l == 0 && a.rstd) a.rstd[row] = r * scale;
 }
 
-// Bound by reading x and the residual and writing their sum and y.  Every lane requests R rows one after the other before it needs the first.  232965 x 128 bf16 with residual 37 us (6.4 TB/s),
-// without 19.8 (6.0), 56944 x 251 fp32 20.0 (5.7).  In 8 bits 232965 x 256 bf16 with residual 75 us (5.6), 56944 x 251 fp32 16.5 (4.4: nine tenths of the time instructions issue).
+// Bound by reading x and the residual and writing their sum and y.  Every lane requests R rows one after the other before it needs the first.  232965 x 128 bf16 with residual 38 us (6.2 TB/s),
+// without 19.8 (6.0), 56944 x 251 fp32 20.0 (5.7).  In 8 bits 232965 x 256 bf16 with residual 75 us (5.6), 56944 x 251 fp32 16.5 (4.4: instructions issue five sixths of the time).
 template <typename T, int LPR, int K, int R, bool TAIL, bool OUT8>
 __global__ __launch_bounds__(kNormBlock<LPR>) void rms_kernel(RmsArgs a) {
     __shared__ float2 lds[2][16];
