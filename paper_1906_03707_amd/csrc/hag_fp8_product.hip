@@ -2,8 +2,9 @@
 // The rows of w are the matrix instructions' rows, so a lane gets four consecutive columns of y.
 // A result of 16 bits takes the elements as they are, 128 columns at a time (v_mfma_scale_f32_16x16x128_f8f6f4): lane l brings, of row l % 16 of either operand, columns 16 q .. 16 q + 15 and
 // 64 + 16 q .. 79 + 16 q, q = l / 16, and the scale of columns 32 q .. 32 q + 31.  Sums are kept in fp32, but before they are added the 8 products that a lane brings next to each other
-// are cut off at 2^-14 of the largest of them (measured: randn operands are off by 1.5e-5 of the result's norm, 5e-5 where elements differ by powers of e^2; the
-// instruction for 32 columns without scales is the same): nothing beside the rounding to 8 or 11 bits.
+// are cut off at 2^-13 of the power of two of the largest of them, an element below 2^-6 of its scale counting as 2^-6 (measured: randn operands are off by 1.5e-5 of the result's norm, 5e-5
+// where elements differ by powers of e^2; the instruction for 32 columns without scales is the same): little beside the rounding to 8 or 11 bits, and for small elements 2^-9 of what their own
+// rounding, to 2^-10 of the scale, left off.
 // An fp32 result takes them as bf16 numbers, which hold an element times its scale exactly, 32 columns at a time (v_mfma_f32_16x16x32_bf16): products are exact, sums as good as in fp32 one
 // by one (5e-8 and 3e-7 of the norm at 2048 columns), at half of the rate.  Which columns meet in an instruction is free, so lanes bring the same 16 columns either way.
 #include "hag_fp8.hpp"

@@ -172,3 +172,27 @@ def test_captured_and_on_another_stream(B):
     here = run()                                           # two calls at once
     side.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(got, here))
+
+
+@pytest.mark.parametrize("n,d,k", [(130, 1, 70), (200, 3, 1900), (40, 8, 40), (17, 33, 300), (300, 128, 300), (700, 300, 900)])
+def test_small_elements_beside_large_ones(B, n, d, k):
+    """Codes of all sizes, those without a leading bit among them: they count as 2^-6 of their scale where products of 16 bits' results are cut off, and are exact for fp32."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+
+    def codes(rows):
+        c = torch.randint(0, 256, (rows, (d + 15) // 16 * 16), dtype=torch.uint8, device="cuda", generator=gen)
+        c = torch.where(torch.rand(c.shape, device="cuda", generator=gen) < 0.3, c & 0x87, c)          # below 2^-6
+        c = torch.where((c & 0x7f) == 0x7f, c - 7, c)
+        return c.view(E4M3)[:, :d], torch.randint(118, 122, (rows, (d + 31) // 32), dtype=torch.uint8, device="cuda", generator=gen).view(E8M0)
+
+    (x, xs), (w, ws) = codes(n), codes(k)
+    check(B.fp8_product(x, xs, w, ws), x, xs, w, ws, torch.float32)
+    a, b = wide(x, xs), wide(w, ws).t().contiguous()
+    want = a @ b
+    least = [2.0 ** -6 * s.double().repeat_interleave(32, 1)[:, :d] for s in (xs, ws)]
+    size = torch.maximum(a.abs(), least[0]) @ torch.maximum(b.abs(), least[1].t()).contiguous()
+    # each of up to 16 neighbours may lose 2^-13 of the largest of them, which is less than the sum of their sizes
+    bound = ((d + 2) * EPS + 16 * 2.0 ** -13) * size
+    for dtype in (torch.bfloat16, torch.float16):
+        y = B.fp8_product(x, xs, w, ws, dtype=dtype).double()
+        assert bool(((y - want).abs() <= bound + HALF[dtype] * (want.abs() + bound) + TINY[dtype])[want.abs() + bound < 60000].all())
