@@ -219,8 +219,11 @@ def _free_ended(*more):
     _ended.extend(more)
     torch = sys.modules.get("torch")
     if _ended and not (torch is not None and torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing()):
-        while _ended:
-            free, handle = _ended.pop()
+        while True:
+            try:
+                free, handle = _ended.pop()
+            except IndexError:                  # (or another thread's, or garbage collected meanwhile)
+                return
             free(handle)
 
 
