@@ -166,7 +166,9 @@ class _RmsNorm(torch.autograd.Function):
 
 def rms_norm(x, weight=None, eps=1e-5, residual=None):
     """h / sqrt(mean of h^2 + eps) * weight over the last dimension of h = x + residual (float32, bfloat16 or float16, both alike), weight [d] of that type or float32.  With a residual
-    (y, h): h goes on to the next layer, past what is computed from y.  Its backward pass is not itself differentiable."""
+    (y, h): h goes on to the next layer, past what is computed from y; the residual has the shape of x, nothing is broadcast.  Its backward pass is not itself differentiable."""
+    if residual is not None and residual.shape != x.shape:      # (as matrices of rows they might match all the same)
+        raise ValueError(f"residual must have the shape of x {tuple(x.shape)}, got {tuple(residual.shape)}")
     return _RmsNorm.apply(x, weight, eps, residual)
 
 
