@@ -172,8 +172,10 @@ def rms_norm(x, weight=None, eps=1e-5, residual=None):
     return _RmsNorm.apply(x, weight, eps, residual)
 
 
+@torch.no_grad()
 def quantize_fp8(w):
-    """Rows [k, d] in 8 bits, as rms_norm_fp8 leaves them: (codes, scales), a power of two for every 32 columns, elements to the nearest.  Plain torch: for weights, once."""
+    """Rows [k, d] in 8 bits, as rms_norm_fp8 leaves them: (codes, scales), a power of two for every 32 columns, elements to the nearest.  Plain torch: for weights, once; no gradient
+    goes through it."""
     k, d = w.shape
     w = w.float()
     most = torch.nn.functional.pad(torch.where(w.isfinite(), w.abs(), 0.0), (0, -d % 32)).reshape(k, (d + 31) // 32, 32).amax(2)

@@ -12,3 +12,12 @@ def test_norm_refuses_a_residual_of_another_shape(shape):
     for a, b in ((x, torch.ones(shape)), (torch.ones(shape), x)):
         with pytest.raises(ValueError, match="residual"):
             layers.rms_norm(a, residual=b)
+
+
+def test_quantized_rows_of_a_parameter_are_apart_from_it():
+    from paper_1906_03707_amd import layers
+    w = torch.nn.Parameter(torch.randn(5, 40, generator=torch.Generator().manual_seed(1)))
+    codes, scales = layers.quantize_fp8(w)
+    assert not codes.requires_grad and codes.grad_fn is None and not scales.requires_grad
+    want, want_scales = layers.quantize_fp8(w.detach())
+    assert torch.equal(codes.float(), want.float()) and torch.equal(scales.float(), want_scales.float())
