@@ -230,6 +230,9 @@ __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(Produc
     auto turn = [&](int step, bytes16_t *codes, uint32_t *scales, const uint32_t (&scale)[SCALES], bytes16_t *next, uint32_t (&next_scale)[SCALES]) {
         if (step + 1 == steps && a.d % 16) cut(step, codes);
         keep_scales(scales, scale);
+        // A wavefront's own pieces have to be in LDS before the barrier lets the others read them.  Said here: a barrier waits for no load by itself, and a wavefront that keeps no scales (128 x 64:
+        // one of four) has none of its own to wait for.
+        __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0), the other counters as they are
         __syncthreads();
         if (step > 0 && step + 1 < steps) request(step + 1, next, next_scale);
         work(codes, scales);
