@@ -465,7 +465,8 @@ int hag_clip_gradients(int64_t tensors, const hag_tensor_t *list, double max_nor
  * 16 bits are rounded once a step; `copy` (may be NULL) gets the new parameters in copy_dtype: 16 bits to compute with beside HAG_F32 ones that are trained.  Gradients of HAG_F32
  * parameters may be of any type, of others are of theirs.  bits 32: m and v are fp32.  bits 8: m and, in the place of v, its root, both in 8 bits as above, in blocks of 32 consecutive
  * elements; they are rounded up or down by chance, so that their mean is kept, by a hash of seed, step and the element's number in its tensor: the same call gives the same bits.
- * Squares of gradients are taken in fp32: they count up to 1e19.  `list` is host memory, read during the call.  lr_device (fp32) and step_device (HAG_I64, at least 1; both may be NULL) take
+ * eps is in 2^-126 .. 2^100.  Squares of gradients are taken in fp32: they count up to 1e19, and below 2^-126 they lose bits, which puts a root, as it stands beside eps, off by
+ * 5e-23 / sqrt(1 - beta2) at most (1.5e-21 for 0.999).  `list` is host memory, read during the call.  lr_device (fp32) and step_device (HAG_I64, at least 1; both may be NULL) take
  * the place of lr and step, for calls that are captured and replayed.  Tensors must not overlap. */
 int hag_rms_norm(int64_t n, int64_t d, hag_dtype_t dtype, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, hag_dtype_t param_dtype, const void *weight,
                  float eps, void *h, void *y, float *rstd, void *stream);

@@ -121,12 +121,20 @@ __device__ __forceinline__ uint32_t dithered(float v, uint32_t byte, uint32_t ra
     return (__float_as_uint(ldexpf(fabsf(v), 7 - (int)byte)) + random) >> 20;         // 127 - byte - 120
 }
 
-// The root rounded correctly, as IEEE's: the hardware's is at most one unit off, and the remainders at the numbers beside it say which way.  (Below 2^-100 those lose bits, and it is as
-// good as the hardware's.)
+// Squares below 2^-126 have a root that counts where eps is smaller still, and the hardware's root takes them for zeros: numbers below 2^-96 are taken times 2^64, their roots times 2^-32,
+// both exact.
+constexpr float kRootLeast = 0x1p-96f, kRootUp = 0x1p64f, kRootBack = 0x1p-32f;
+__device__ __forceinline__ float near_root(float x) {
+    const bool least = x < kRootLeast;
+    return __builtin_amdgcn_sqrtf(least ? x * kRootUp : x) * (least ? kRootBack : 1.f);
+}
+// The root rounded correctly, as IEEE's, by Tuckerman's test: s is right if s (s - u) < x <= s (s + u) for the numbers s - u and s + u beside it, and the hardware's is at most one of them off.
 __device__ __forceinline__ float root_of(float x) {
-    const float s = __builtin_amdgcn_sqrtf(x), down = __uint_as_float(__float_as_uint(s) - 1u), up = __uint_as_float(__float_as_uint(s) + 1u);
-    const float r = fmaf(-down, s, x) <= 0.f ? down : s;   // (of zero, infinity and no number: comparisons with no number, s stays)
-    return fmaf(-up, s, x) > 0.f ? up : r;
+    const bool least = x < kRootLeast;
+    const float of = least ? x * kRootUp : x, s = __builtin_amdgcn_sqrtf(of), down = __uint_as_float(__float_as_uint(s) - 1u), up = __uint_as_float(__float_as_uint(s) + 1u);
+    float r = fmaf(-down, s, of) <= 0.f ? down : s;        // (of zero, infinity and no number: comparisons with no number, s stays)
+    r = fmaf(-up, s, of) > 0.f ? up : r;
+    return r * (least ? kRootBack : 1.f);
 }
 
 // Four elements of a tensor, `have` of them there (FULL: all), as they come from memory: elements at + mine and on, `at` the workgroup's, a multiple of 1024.  Eight adjacent lanes have a
@@ -176,7 +184,7 @@ struct AdamFour {
                 root = nv[e] = root_of(a.b2 * (nv[e] * nv[e]) + a.a2 * (d * d));
             } else {
                 nv[e] = a.b2 * v[e] + a.a2 * (d * d);
-                root = __builtin_amdgcn_sqrtf(nv[e]);      // (one unit in the last place, as the reciprocal)
+                root = near_root(nv[e]);                   // (one unit in the last place, as the reciprocal)
             }
             np[e] = fmaf(-a.rate, nm[e] * __builtin_amdgcn_rcpf(fmaf(root, a.root, a.eps)), (float)p[e] * a.keep);
         }
