@@ -199,17 +199,26 @@ def clip_gradients(parameters, max_norm):
 
 def _no_capture():
     if torch.cuda.is_current_stream_capturing():
-        raise RuntimeError("an optimiser's step counts on the host and cannot be captured: binding.adamw takes the number from the device")
+        raise RuntimeError("an optimiser's step cannot be captured, its replays would all have its number: binding.adamw takes the number from the device")
 
 
 class AdamW:
     """AdamW (hag_adamw) for float32, bfloat16 or float16 leaves.  bits: of its states, 32 (two float32 numbers for each element) or 8 (two bytes and a sixteenth, rounded by chance from `seed` and
-    the step so that their means are kept).  lr may be changed between steps; one count of steps for all parameters.  A step is not captured into a graph, whose replays would all have its
-    number: binding.adamw takes the number, and lr, from the device."""
+    the step so that their means are kept).  lr may be changed between steps; one count of steps for all parameters, `steps`, which leaves out those that changed nothing (to read it waits for
+    the device once a step has been clipped).  A step is not captured into a graph, whose replays would all have its number: binding.adamw takes the number, and lr, from the device."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, seed=0):
-        self.params, self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.seed, self.steps = list(params), lr, betas, eps, weight_decay, bits, seed, 0
+        self.params, self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.seed = list(params), lr, betas, eps, weight_decay, bits, seed
         self.states = binding.adamw_states(self.params, bits)
+        self._count = 0                                    # a number until a norm may have left a step out, then one on the device: nothing waits for it
+
+    @property
+    def steps(self):
+        return int(self._count)
+
+    @steps.setter
+    def steps(self, count):
+        self._count = count
 
     def zero_grad(self):
         for p in self.params:
@@ -217,17 +226,18 @@ class AdamW:
 
     def step(self, max_norm=None):
         """One step on the parameters that have a gradient.  max_norm: as if their gradients were scaled down to that norm, which they are not; the norm they have, a float32 scalar on
-        the device, is returned (nothing waits for it), and where it is no finite number no parameter and no state changes (a NaN among the gradients makes all of them NaN)."""
+        the device, is returned (nothing waits for it), and where it is no finite number no parameter and no state changes, nor the count (a NaN among the gradients makes all of them NaN)."""
         _no_capture()
         at = [i for i, p in enumerate(self.params) if p.grad is not None]
         params = [self.params[i] for i in at]
         grads = [p.grad if p.grad.stride() == p.stride() or p.is_contiguous() and p.grad.is_contiguous() else torch.empty_like(p, dtype=p.grad.dtype).copy_(p.grad) for p in params]
         norm = None if max_norm is None else binding.clip_gradients(grads, float("inf"))
         if params:
-            binding.adamw([p.detach() for p in params], grads, **{k: [x[i] for i in at] for k, x in self.states.items()}, step=self.steps + 1, lr=self.lr, betas=self.betas, eps=self.eps,
+            count = self._count + (1 if norm is None else norm < float("inf"))     # (norms have no sign; the step's number where it is made)
+            binding.adamw([p.detach() for p in params], grads, **{k: [x[i] for i in at] for k, x in self.states.items()}, step=count, lr=self.lr, betas=self.betas, eps=self.eps,
                           weight_decay=self.weight_decay, norm=norm, max_norm=max_norm, seed=self.seed)
             torch.autograd.graph.increment_version(params)
-            self.steps += 1
+            self._count = count
         return norm
 
     def state_dict(self):
