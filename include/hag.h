@@ -249,6 +249,7 @@ int hag_seq_lstm_backward(const hag_seq_t *h, int64_t d, int64_t hidden, const f
                           const float *g_a, float *g_x, float *g_w_ih, float *g_w_hh, float *g_b, void *workspace,
                           void *stream);
 
+/* hag_free, hag_seq_free: also while a stream is captured, by this thread or another: the capture goes on. */
 void hag_free(hag_t *h);
 
 int hag_stats(const hag_t *h, hag_stats_t *out);

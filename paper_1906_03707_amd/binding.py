@@ -215,7 +215,8 @@ _ended = []                                 # (free, handle) of objects that are
 
 
 def _free_ended(*more):
-    """Frees the handles of objects that are gone; not while a graph is captured, which giving memory back would break (garbage is collected at any time): with the next ones then."""
+    """Frees the handles of objects that are gone.  Garbage is collected at any time: while this thread's stream is captured they wait, for the next ones or the next call of a handle (what other
+    threads and streams capture is left alone by hag_free itself)."""
     _ended.extend(more)
     torch = sys.modules.get("torch")
     if _ended and not (torch is not None and torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing()):
@@ -344,6 +345,8 @@ class Hag:
         # A call on a small graph takes about as long as preparing it, so everything that depends on sizes only is looked up, and
         # the stream is asked for once.
         import torch
+        if _ended:
+            _free_ended()
         op_code, code, d, nbytes, forward_nbytes = self._shape(what, a, op)
         if out is not None or argmax is not None or workspace is not None or needs_argmax:
             self._check_args(what, a, op, out, argmax, workspace, needs_argmax)
@@ -995,6 +998,7 @@ class SeqHag:
                 take(lp, nl.value + 1, np.int64), take(fs, self.n, np.int32))
 
     def upload(self):
+        _free_ended()
         _check(lib().hag_seq_upload(self._h))
         return self
 
@@ -1008,6 +1012,8 @@ class SeqHag:
     def lstm_forward_train(self, x, w_ih, w_hh, b, workspace=None):
         """As lstm_forward, keeping what lstm_backward needs; returns (a [n, H], workspace)."""
         import torch
+        if _ended:
+            _free_ended()
         hidden, d = int(w_hh.shape[1]), int(x.shape[1])
         for name, t, shape in (("x", x, (self.n, d)), ("w_ih", w_ih, (4 * hidden, d)), ("w_hh", w_hh, (4 * hidden, hidden)),
                                ("b", b, (4 * hidden,))):
@@ -1053,6 +1059,8 @@ class SeqHag:
     def lstm_forward(self, x, w_ih, w_hh, b, out=None, workspace=None):
         """a [n, H] = LSTM aggregate of every node's ordered list; torch float32 device tensors."""
         import torch
+        if _ended:
+            _free_ended()
         hidden, d = int(w_hh.shape[1]), int(x.shape[1])
         for name, t, shape in (("x", x, (self.n, d)), ("w_ih", w_ih, (4 * hidden, d)), ("w_hh", w_hh, (4 * hidden, hidden)),
                                ("b", b, (4 * hidden,))):

@@ -677,6 +677,7 @@ static int upload_plan(hag_handle *h, Plan &p, hipStream_t s) {
 
 void free_device(hag_handle *h) {
     if (!h->d_allocs.empty()) {
+        const BesideCaptures beside;
         int cur = -1;
         bool sw = hipGetDevice(&cur) == hipSuccess && h->device >= 0 && cur != h->device;
         if (sw) (void)hipSetDevice(h->device);

@@ -13,6 +13,15 @@
 
 namespace hag {
 
+// Giving device memory back breaks a capture that is under way on any thread (handles are freed whenever their owner's garbage is collected), unless the thread that gives it back has
+// said that it does not take part: its mode while such an object lives.
+struct BesideCaptures {
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    BesideCaptures() { (void)hipThreadExchangeStreamCaptureMode(&mode); }
+    ~BesideCaptures() { (void)hipThreadExchangeStreamCaptureMode(&mode); }
+    BesideCaptures(const BesideCaptures &) = delete;
+};
+
 // R_SUMIF: sum of the rows' elements whose entry in a second, int32 matrix (GatherArgs::filter, same
 // shape and row index as src_lo) equals the id of the output row: the backward pass of max as a
 // gather, gx[u, f] = sum over consumers v of u of gy[v, f] where argmax[v, f] == u, in a fixed order

@@ -2189,17 +2189,11 @@ int hag_seq_create(int64_t n, const int64_t *rowptr, const int32_t *col, int64_t
 
 void hag_seq_free(hag_seq_t *h) {
     if (!h) return;
-    if (h->d_final) (void)hipFree(h->d_final);
-    if (h->d_paths) (void)hipFree(h->d_paths);
-    if (h->d_paths_by_depth) (void)hipFree(h->d_paths_by_depth);
-    if (h->d_xt_prev) (void)hipFree(h->d_xt_prev);
-    if (h->d_xt_seg) (void)hipFree(h->d_xt_seg);
-    if (h->d_used) (void)hipFree(h->d_used);
-    if (h->d_step_g) (void)hipFree(h->d_step_g);
-    if (h->d_xt_idx) (void)hipFree(h->d_xt_idx);
-    if (h->d_pending_init) (void)hipFree(h->d_pending_init);
-    if (h->d_step_out) (void)hipFree(h->d_step_out);
-    if (h->d_gave_up) (void)hipFree(h->d_gave_up);
+    if (h->d_paths) {                                      // (the first of them)
+        const BesideCaptures beside;
+        for (int32_t *p : {h->d_final, h->d_paths, h->d_paths_by_depth, h->d_xt_prev, h->d_xt_seg, h->d_used, h->d_step_g, h->d_xt_idx, h->d_pending_init, h->d_step_out, h->d_gave_up})
+            if (p) (void)hipFree(p);
+    }
     delete h;
 }
 
