@@ -458,7 +458,8 @@ int hag_clip_gradients(int64_t tensors, const hag_tensor_t *list, double max_nor
  *
  * hag_fp8_product: y [n, k] = x w^T for x [n, d] and w [k, d] in 8 bits, with scales as above (255: no number) and strides in bytes; k at most 2^20; y of `dtype`, summed in fp32.  For
  * HAG_F32 products are exact (elements that are with their scale below 2^-126 may count as 0, above 2^128 as infinite); for 16 bits a product may be cut off at 2^-13 of the largest
- * of 8 or 16 neighbours, as the matrix cores do, elements below 2^-6 of their scale counting as that much for which is the largest.
+ * of 8 or 16 neighbours, as the matrix cores do, elements below 2^-6 of their scale counting as that much for which is the largest.  Many rows are several times as fast where those of both
+ * begin at multiples of 16 bytes.
  *
  * hag_adamw: one step, in place, of
  *   g' = c g, m = beta1 m + (1 - beta1) g', v = beta2 v + (1 - beta2) g'^2, p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)

@@ -792,7 +792,9 @@ def _rows_fp8(name, codes, scales, device):
 
 
 def fp8_product(x, x_scales, w, w_scales, dtype=None):
-    """x w^T [n, k] of rows in 8 bits, x [n, d] and w [k, d] as rms_norm_fp8 and layers.quantize_fp8 give them; dtype: float32 (the default), bfloat16 or float16 (hag_fp8_product)."""
+    """x w^T [n, k] of rows in 8 bits, x [n, d] and w [k, d] as rms_norm_fp8 and layers.quantize_fp8 give them; dtype: float32 (the default), bfloat16 or float16 (hag_fp8_product).
+
+    float32 adds up exact products.  For 16 bits products lose what is below 2^-13 of the largest of their neighbours: 1.5e-5 to 5e-5 of the result's norm, before it is rounded (2^-8 or 2^-11)."""
     import torch
     device = _device()
     dtype = torch.float32 if dtype is None else dtype

@@ -222,7 +222,8 @@ struct AdamFour {
         }
         const uint32_t byte_m = scale_byte(lanes_max<8>(__uint_as_float(most_m))), byte_v = scale_byte(lanes_max<8>(__uint_as_float(most_v)));
         uint32_t codes_m = 0, codes_v = 0;
-        const uint32_t place = ((uint32_t)at + mine) * 0x9e3779b1u + a.key + (uint32_t)(at >> 32) * 0x85ebca6bu;    // (a piece does not cross 2^32)
+        // (multiples of the prime next to 2^32 divided by the golden ratio, Knuth's choice for multiplicative hashing; of any odd number from 2^32 on.  A piece does not cross 2^32)
+        const uint32_t place = ((uint32_t)at + mine) * 0x9e3779b1u + a.key + (uint32_t)(at >> 32) * 0x85ebca6bu;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint32_t random = mixed(place + (uint32_t)e * 0x9e3779b1u);
@@ -267,7 +268,7 @@ __device__ __forceinline__ void adam_unit(const AdamArgs::Tensor &t, const AdamN
 }
 
 // Bound by moving parameters, gradients and states: 30 M fp32 parameters with states in 32 bits 167 us (28 bytes each, 5.0 TB/s; one or four pieces on their way 167 and 165, streaming stores
-// 168), in 8 bits with bf16 gradients and copies 101 (16.1 bytes, 4.8; 75 vector instructions an element, which issue for seven tenths of the time, 12 of them the hash).
+// 168), in 8 bits with bf16 gradients and copies 101 (16.1 bytes, 4.8; 80 vector instructions an element, which issue for three quarters of the time, 12 of them the hash).
 template <int BITS>
 __global__ __launch_bounds__(kBlock) void adamw_kernel(AdamArgs a) {
     AdamNumbers s;

@@ -121,11 +121,14 @@ struct ProductTiles {
 // A workgroup takes TM rows of x and TN of w, its wavefronts WR times WC parts of them.  128 columns of both are on their way from memory to LDS, past the registers, while the 128 before are
 // multiplied; the first two sets are requested together.  What LDS holds and the registers' sums limit the tile: 256 x 256 for results of 16 bits (64 KB for 128 columns, two of them; 128
 // registers of sums).
-// 131072 x 1024 x 1024 into bf16 200 us (1.4 PFLOP/s; the library's bf16 product of these sizes 307 us), without the products 190, without the stores 142, without the loads 163: loads come 2 us
-// after they are asked for, and only as much is on its way as LDS has room for.  128 columns as two 64s, so that two workgroups fit a compute unit, took 266 (lines of 128 bytes are asked for
-// twice, what L2 answers per clock), one workgroup that goes from tile to tile and asks for the next one's first columns early 212, tiles of 128 x 128 259.
-// Narrow results are bound by memory: 232965 x 128 x 128 into bf16 17.7 us (5.1 TB/s), into fp32 29.5 (5.1), 56944 x 251 x 74 into fp32 10.9 (2.9: a load's way, a product's, a store's).
-// fp32 results convert in registers: 131072 x 1024 x 1024 362 us (0.76 PFLOP/s; with the next piece converted between the products of the present one 364), 16384 x 2048 x 2048 148 (0.93).
+// 131072 x 1024 x 1024 into bf16 186 us in hundreds of passes without a pause (1.48 PFLOP/s; the library's bf16 product of these sizes 253 us), 204 in 15 passes after one (303).  Of 200 in such
+// short runs it takes 190 without the products, 142 without the stores, 163 without the loads: loads come 2 us after they are asked for, and only as much is on its way as LDS has room for.
+// There, 128 columns as two 64s, so that two workgroups fit a compute unit, took 266 (lines of 128 bytes are asked for twice, what L2 answers per clock), one workgroup that goes from tile to
+// tile and asks for the next one's first columns early 212, tiles of 128 x 128 259.
+// Narrow results are bound by memory (without pauses): 232965 x 128 x 128 into bf16 17.3 us (5.2 TB/s), into fp32 28.0 (5.4), 56944 x 251 x 74 into fp32 11.5 (2.8: a load's way, a product's, a
+// store's).
+// fp32 results convert in registers: 131072 x 1024 x 1024 326 us without pauses (0.84 PFLOP/s), 390 after one (in one run 362, and 364 with the next piece converted between the products of the
+// present one), 16384 x 2048 x 2048 134 (1.02) and 153.
 template <typename O, int TM, int TN, int WR, int WC>
 __global__ __launch_bounds__(kWave * WR * WC, 2) void product_tile_kernel(ProductTiles args) {
     constexpr bool WIDE = sizeof(O) == 4;
@@ -429,6 +432,8 @@ int hag_fp8_product(int64_t n, int64_t d, int64_t k, const uint8_t *x, int64_t x
         // Few workgroups: as small as they come.  64 x 2048 x 2048 into bf16: 16 rows of x each 6.8 us, 32 7.8, 64 10.8 (1 x 512 x 512 3.3, 1 x 2048 x 2048 5.5).  Up to some bytes to read
         // again they still beat tiles, which wait for memory once per 128 columns: 3000 x 2048 x 64 16 rows 10.9, 32 7.9, 64 10.8, tiles 13.6; 2000 x 256 x 256 4.2, 3.8, 3.9, 4.6;
         // 1000 x 2048 x 300 15.8, 13.1, 11.1, 14.0; but 2048 x 512 x 512 10.5, 7.9, 6.9, 6.2 and 300 x 2048 x 2048 25.9, 19.3, 20.8, 14.4.
+        // Few rows of x and very many of w are tiles too: 1 x 4096 x 131072 into fp32 143 us, into bf16 125 (0.55 GB: 104).  Many rows at any address read x again for every 32 columns of y, without a
+        // pause 56944 x 251 x 74 into fp32 43 us (at multiples of 16: 11.5), 232965 x 128 x 128 into bf16 109 (17.3), 131072 x 1024 x 1024 3.4 ms (186 us): whoever lays them out begins them at those.
         const int64_t groups = (k + 31) / 32, tiles = ((n + 127) / 128) * ((k + 127) / 128);
         if ((n + 15) / 16 * groups <= 256) return launch_split<O, 1>(a, s);
         if (tiles <= 64 && (n + 31) / 32 * groups * d <= 400000) return launch_split<O, 2>(a, s);
