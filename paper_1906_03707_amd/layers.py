@@ -210,7 +210,7 @@ class AdamW:
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, seed=0):
         self.params, self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.seed = list(params), lr, betas, eps, weight_decay, bits, seed
         self.states = binding.adamw_states(self.params, bits)
-        self._count = 0                                    # a number until a norm may have left a step out, then one on the device: nothing waits for it
+        self._count = self._next = 0                       # a number until a norm may have left a step out, then one on the device: nothing waits for it
 
     @property
     def steps(self):
@@ -218,7 +218,16 @@ class AdamW:
 
     @steps.setter
     def steps(self, count):
-        self._count = count
+        self._count = int(count)
+
+    def _number(self, norm):
+        """The number of the next step, which the norm of its gradients may leave out.  On the device it goes from one of two tensors to the other: both stay where they are, so that steps on
+        one stream and then another need no more order than the states do."""
+        if isinstance(self._count, int):
+            if norm is None:
+                return self._count + 1
+            self._count, self._next = (torch.full((), self._count, dtype=torch.int64, device=norm.device) for _ in range(2))
+        return torch.add(self._count, 1 if norm is None else norm < float("inf"), out=self._next)          # (norms have no sign)
 
     def zero_grad(self):
         for p in self.params:
@@ -233,11 +242,11 @@ class AdamW:
         grads = [p.grad if p.grad.stride() == p.stride() or p.is_contiguous() and p.grad.is_contiguous() else torch.empty_like(p, dtype=p.grad.dtype).copy_(p.grad) for p in params]
         norm = None if max_norm is None else binding.clip_gradients(grads, float("inf"))
         if params:
-            count = self._count + (1 if norm is None else norm < float("inf"))     # (norms have no sign; the step's number where it is made)
+            count = self._number(norm)
             binding.adamw([p.detach() for p in params], grads, **{k: [x[i] for i in at] for k, x in self.states.items()}, step=count, lr=self.lr, betas=self.betas, eps=self.eps,
                           weight_decay=self.weight_decay, norm=norm, max_norm=max_norm, seed=self.seed)
             torch.autograd.graph.increment_version(params)
-            self._count = count
+            self._count, self._next = count, self._count
         return norm
 
     def state_dict(self):

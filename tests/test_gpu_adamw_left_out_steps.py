@@ -88,3 +88,33 @@ def test_count_may_be_set_and_a_failed_call_does_not_count(B):
     with pytest.raises(B.HagError):
         opt.step()
     assert opt.steps == 5
+
+
+def test_steps_on_two_streams(B):
+    """Steps in turn on two streams, each waiting for the one before, while the other stream goes on with work of its own: the count's memory is not given to that."""
+    from paper_1906_03707_amd import layers
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    first = start(gen)
+    ours, plain = (layers.AdamW([p.clone().requires_grad_() for p in first], lr=0.01, weight_decay=0.1) for _ in range(2))
+    streams, places = [torch.cuda.current_stream(), torch.cuda.Stream()], set()
+    grads = [[torch.randn(p.shape, device="cuda", generator=gen) for p in first] for _ in range(6)]
+    busy = torch.ones(1 << 24, device="cuda")
+    for k, gs in enumerate(grads):
+        if k == 3:
+            gs[0][0, 0] = math.inf
+        for p, q, g in zip(ours.params, plain.params, gs):
+            p.grad, q.grad = g.clone(), g.clone()
+        here, other = streams[k % 2], streams[1 - k % 2]
+        here.wait_stream(other)
+        with torch.cuda.stream(here):
+            for _ in range(10):
+                busy.mul_(1.0)
+            ours.step(max_norm=1.0)
+            places.add(ours._count.data_ptr())
+        with torch.cuda.stream(other):
+            for _ in range(20):
+                torch.full((), -7, dtype=torch.int64, device="cuda")
+        torch.cuda.synchronize()
+        if k != 3:
+            plain.step(max_norm=1.0)
+    assert same(ours, plain) and ours.steps == plain.steps == 5 and len(places) == 2
